@@ -330,6 +330,80 @@ kf_status kf_decode_select_step_noalloc(kf_cache *c, const void *q, const void *
                                         int32_t k, int32_t w, int32_t layout, int32_t *kept_idx,
                                         int32_t *skipped, void *stream);
 
+/*
+ * Rows of a projection on their way to the calls above, in one pass: per-head norm of queries and keys, position
+ * rotation, and the turn from token-major to head-major rows.  For every sequence b, token t and head
+ *     x' = x / sqrt(mean(x^2) + eps) * weight            queries and keys, where a weight is given
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t)   queries and keys, t = position * inv_freq[i]
+ * for the pairs i < rot_dim/2 of the row's first rot_dim elements; the other elements, and values, pass as they are.
+ * The position of token t is pos0 + t, or seq_pos[b] + t.  Everything is computed in 32 bits (angles in 64) and rounded
+ * once to the element type.
+ *   q, k, v : DEVICE, head h of token (b, t) begins at element b*stride[0] + t*stride[1] + h*d: q has H*q_per_kv
+ *             heads, k and v have H.  A stride pair of zeros means contiguous rows.  One fused projection is three
+ *             pointers into the same rows with the same strides.
+ *   Q       : DEVICE [B][H*q_per_kv][n][d], as kf_prefill_score takes it; with n = 1 the q of kf_decode_step.
+ *   K, V    : DEVICE [B][H][kv_rows][d]; rows [0, n) are written.  A layer of a cache (kv_rows = cap), or, with
+ *             n = kv_rows = 1, the k_new and v_new of kf_decode_step.
+ * Inputs and outputs share one element type (that of the cache, not a 4-bit one) and must not overlap.  Any of the
+ * three pairs (q, Q), (k, K), (v, V) may be left out, both NULL.
+ * With seq_n, rows seq_n[b]..n-1 of sequence b are padding: neither read nor written; a sequence whose seq_n[b]
+ * lies outside [1, n] is left out.
+ * Errors: KF_EINVAL for sizes, strides, alignment (all pointers and strides: 16 bytes), a pair half given, no pair
+ * given, eps not finite or negative, a rotation without inv_freq or with rot_dim odd or outside [2, d].
+ */
+typedef enum { KF_ROTATE_NONE = 0, KF_ROTATE_PAIRS = 1 /* (2i, 2i+1) */, KF_ROTATE_HALVES = 2 /* (i, i + rot_dim/2) */ } kf_rotation;
+typedef struct {
+    int32_t B, n, H, q_per_kv, d, dtype; /* as in kf_cache; q_per_kv 0 means 1, any other positive number is served */
+    int32_t kv_rows;                     /* rows a head of K and V has room for, at least n   */
+    int64_t q_stride[2], k_stride[2], v_stride[2]; /* elements between sequences, between tokens */
+    const void *q_weight, *k_weight;     /* DEVICE [d] norm weights in the element type, or NULL: no norm */
+    float eps;
+    int32_t rotate;                      /* kf_rotation                                        */
+    int32_t rot_dim;
+    const float *inv_freq;               /* DEVICE [rot_dim/2] radians a position              */
+    int32_t pos0;
+    const int32_t *seq_pos;              /* DEVICE [B] or NULL                                 */
+    const int32_t *seq_n;                /* DEVICE [B] or NULL                                 */
+} kf_rows;
+kf_status kf_norm_rotate(const kf_rows *r, const void *q, const void *k, const void *v, void *Q, void *K, void *V,
+                         void *stream);
+
+/*
+ * The choice of a beam search, numbered so that kf_beam_fork can take it.  Row r*W + i of the batch is beam i of
+ * request r.  A continuation of beam i by word v has
+ *     total(i, v) = score[i] + x[i][v] - log(sum_v exp x[i][v])
+ * and each request keeps its W best: larger totals first, of equal ones the lower beam, then the larger logit, then
+ * the lower word.  A total that is not a number counts as minus infinity (so a row with a NaN, or of nothing but minus
+ * infinities, is the last choice); in the order of logits a NaN counts as minus infinity.  A beam with done[] set has
+ * reached its end: it goes on as it is, by one continuation, `eos`, at its own score, and its logits are not read.
+ * The best continuation of a beam keeps the beam's row; the others take, best first, the rows of the beams that
+ * have none, in rising order.  So parent[] fulfils kf_beam_fork's condition.
+ *   logits    : DEVICE [R*W] rows of V, row_stride elements apart, any alignment of whole elements
+ *   score     : DEVICE [R*W] summed log-probabilities (at the first step of a search: 0 for one beam of a request and
+ *               minus infinity for the others)
+ *   done      : DEVICE [R*W] or NULL (none has ended)
+ *   parent    : DEVICE [R*W] row of the batch that the new row continues
+ *   token     : DEVICE [R*W] the word it appends
+ *   new_score : DEVICE [R*W]; may be `score`
+ *   new_done  : DEVICE [R*W] or NULL: the parent had ended, or token == eos; may be `done`
+ *   rank      : DEVICE [R*W] or NULL: place of the row among its request's, 0 the best
+ * W = 1 is greedy decoding.  Statistics and totals are held in 64 bits where they are compared (exponentials have 32:
+ * totals of different beams that differ by less than 2^-19 may change places, alike in every call); new_score is the
+ * total rounded to 32.  The workspace needs no initial contents.
+ * Errors: KF_EINVAL for sizes, null pointers, a row_stride below V, eos outside [0, V) with done or new_done;
+ * KF_EUNSUPPORTED for W > 32 or a vocabulary above 500000; KF_EWORKSPACE.
+ */
+typedef struct {
+    int32_t R, W, V;    /* requests, beams of each, vocabulary                */
+    int32_t dtype;      /* of the logits: KF_F32, KF_BF16 or KF_F16           */
+    int64_t row_stride; /* elements between rows; 0: V                        */
+    int32_t eos;        /* word that ends a hypothesis, or -1                 */
+} kf_beams;
+size_t kf_beam_workspace_bytes(const kf_beams *b);
+kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *score, const int32_t *done,
+                         int32_t *parent, int32_t *token, float *new_score, int32_t *new_done, int32_t *rank,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,13 +17,15 @@ F32, BF16, F16 = 0, 1, 2
 NOISE_NONE, NOISE_GUMBEL, NOISE_GAUSSIAN, NOISE_CONSTANT = 0, 1, 2, 3
 LAYOUT_ORDERED, LAYOUT_SLOT = 0, 1
 POS_ORIGINAL, POS_NEW = 0, 1
+ROTATE_NONE, ROTATE_PAIRS, ROTATE_HALVES = 0, 1, 2
 SCORE_PER_LAYER, SCORE_SHARED = 0, 1
 KF_OK, KF_EINVAL, KF_EUNSUPPORTED, KF_EWORKSPACE, KF_EDEVICE = 0, -1, -2, -3, -4
 
 # every symbol include/keyformer.h declares
 SYMBOLS = ("kf_version", "kf_last_error", "kf_tau", "kf_noise_bits", "kf_workspace_bytes",
            "kf_prefill_score", "kf_decode_step", "kf_select_evict", "kf_select_evict_into", "kf_decode_select_step",
-           "kf_decode_launch_shape", "kf_decode_select_step_at", "kf_beam_fork", "kf_decode_select_step_noalloc")
+           "kf_decode_launch_shape", "kf_decode_select_step_at", "kf_beam_fork", "kf_decode_select_step_noalloc",
+           "kf_norm_rotate", "kf_beam_workspace_bytes", "kf_beam_select")
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -49,6 +51,19 @@ class kf_score_cfg(C.Structure):
 
 class kf_schedule(C.Structure):
     _fields_ = [("n", C.c_int32), ("T", C.c_int32), ("tau_init", C.c_float), ("tau_end", C.c_float)]
+
+
+class kf_rows(C.Structure):
+    _fields_ = [("B", C.c_int32), ("n", C.c_int32), ("H", C.c_int32), ("q_per_kv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("kv_rows", C.c_int32), ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2),
+                ("v_stride", C.c_int64 * 2), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float),
+                ("rotate", C.c_int32), ("rot_dim", C.c_int32), ("inv_freq", C.c_void_p), ("pos0", C.c_int32),
+                ("seq_pos", C.c_void_p), ("seq_n", C.c_void_p)]
+
+
+class kf_beams(C.Structure):
+    _fields_ = [("R", C.c_int32), ("W", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("row_stride", C.c_int64),
+                ("eos", C.c_int32)]
 
 
 _lib = None
@@ -106,6 +121,12 @@ def lib():
         L.kf_decode_select_step_noalloc.argtypes = [C.POINTER(kf_cache), vp, vp, vp, C.c_int32, C.c_int32,
                                                     C.POINTER(kf_score_cfg), vp, C.c_int32, C.c_int32, C.c_int32, vp,
                                                     vp, vp]
+        L.kf_norm_rotate.restype = C.c_int
+        L.kf_norm_rotate.argtypes = [C.POINTER(kf_rows), vp, vp, vp, vp, vp, vp, vp]
+        L.kf_beam_workspace_bytes.restype = C.c_size_t
+        L.kf_beam_workspace_bytes.argtypes = [C.POINTER(kf_beams)]
+        L.kf_beam_select.restype = C.c_int
+        L.kf_beam_select.argtypes = [C.POINTER(kf_beams), vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -301,3 +322,79 @@ def kf_decode_select_step_noalloc(cache: Cache, q, k_new, v_new, q_pos: int, m_h
     _check(lib().kf_decode_select_step_noalloc(C.byref(cs), _ptr(q), _ptr(k_new), _ptr(v_new), q_pos, m_hint,
                                                C.byref(cfg), _ptr(out), k, w, layout, _ptr(kept_idx),
                                                _ptr(skipped), _stream(stream)))
+
+
+@dataclass
+class Rows:
+    """How a projection's rows lie, and what becomes of them (kf_norm_rotate).  Strides: elements between
+    sequences and between tokens, (0, 0) for contiguous rows.  q_weight, k_weight: norm weights [d] in the
+    element type, or None; inv_freq: float32 [rot_dim / 2]; seq_pos, seq_n: int32 [B] or None."""
+    B: int
+    n: int
+    H: int
+    d: int
+    dtype: int
+    q_per_kv: int = 1
+    kv_rows: int = 0       # rows a head of K and V has room for; 0: n
+    q_stride: tuple = (0, 0)
+    k_stride: tuple = (0, 0)
+    v_stride: tuple = (0, 0)
+    q_weight: object = None
+    k_weight: object = None
+    eps: float = 1e-6
+    rotate: int = ROTATE_NONE
+    rot_dim: int = 0
+    inv_freq: object = None
+    pos0: int = 0
+    seq_pos: object = None
+    seq_n: object = None
+
+    def c_struct(self) -> kf_rows:
+        two = C.c_int64 * 2
+        return kf_rows(self.B, self.n, self.H, self.q_per_kv, self.d, self.dtype, self.kv_rows or self.n, two(*self.q_stride),
+                       two(*self.k_stride), two(*self.v_stride), _ptr(self.q_weight), _ptr(self.k_weight), self.eps, self.rotate,
+                       self.rot_dim, _ptr(self.inv_freq), self.pos0, _ptr(self.seq_pos), _ptr(self.seq_n))
+
+
+def kf_norm_rotate(rows: Rows, q, k, v, Q, K, V, stream=None) -> None:
+    """q, k, v: a projection's rows, token by token; Q [B,H*q_per_kv,n,d] and K, V [B,H,kv_rows,d] (a layer of a
+    cache's K and V) receive them head by head.  A pair (q and Q, k and K, v and V) may be None."""
+    cs = rows.c_struct()
+    _check(lib().kf_norm_rotate(C.byref(cs), _ptr(q), _ptr(k), _ptr(v), _ptr(Q), _ptr(K), _ptr(V), _stream(stream)))
+
+
+@dataclass
+class Beams:
+    """Sizes of a beam selection: R requests of W beams, a vocabulary of V words, the logits' element type."""
+    R: int
+    W: int
+    V: int
+    dtype: int = F32
+    row_stride: int = 0    # elements between rows of logits; 0: V
+    eos: int = -1
+
+    def c_struct(self) -> kf_beams:
+        return kf_beams(self.R, self.W, self.V, self.dtype, self.row_stride, self.eos)
+
+
+def kf_beam_workspace_bytes(beams: Beams) -> int:
+    cs = beams.c_struct()
+    return int(lib().kf_beam_workspace_bytes(C.byref(cs)))
+
+
+def new_beam_workspace(beams: Beams, device="cuda"):
+    """A workspace tensor for kf_beam_select with these sizes."""
+    import torch
+    nbytes = kf_beam_workspace_bytes(beams)
+    if nbytes == 0:
+        raise KeyformerError(KF_EUNSUPPORTED, lib().kf_last_error().decode())
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def kf_beam_select(beams: Beams, logits, score, parent, token, new_score, done=None, new_done=None, rank=None, workspace=None,
+                   stream=None) -> None:
+    """logits [R*W, V]; score, new_score float32 [R*W] (may be the same); parent, token, rank, done, new_done int32 [R*W]."""
+    cs = beams.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_beam_select(C.byref(cs), _ptr(logits), _ptr(score), _ptr(done), _ptr(parent), _ptr(token), _ptr(new_score),
+                                _ptr(new_done), _ptr(rank), wp, wb, _stream(stream)))

@@ -791,4 +791,136 @@ kf_status kf_decode_select_step_at(kf_cache* c, const void* q, const void* k_new
                       workspace_bytes, stream);
 }
 
+kf_status kf_norm_rotate(const kf_rows* r, const void* q, const void* k, const void* v, void* Q, void* K, void* V,
+                         void* stream) {
+    if (!r) return fail(KF_EINVAL, "rows description is NULL");
+    if (r->B < 1 || r->n < 1 || r->H < 1 || r->d < 1 || r->q_per_kv < 0)
+        return fail(KF_EINVAL, "sizes must be positive (B=%d n=%d H=%d d=%d q_per_kv=%d)", r->B, r->n, r->H, r->d, r->q_per_kv);
+    if (r->dtype != KF_F32 && r->dtype != KF_BF16 && r->dtype != KF_F16) return fail(KF_EINVAL, "unknown dtype %d", r->dtype);
+    if (!supported(r->dtype, r->d))
+        return fail(KF_EUNSUPPORTED, "dtype %d with head dimension %d is not built", r->dtype, r->d);
+    const int64_t G = r->q_per_kv > 1 ? r->q_per_kv : 1, HQ = r->H * G;
+    if (HQ + 2 * (int64_t)r->H > 1 << 24) return fail(KF_EINVAL, "too many heads");
+    if (!q != !Q || !k != !K || !v != !V) return fail(KF_EINVAL, "an input without its output, or an output without its input");
+    if (!q && !k && !v) return fail(KF_EINVAL, "neither queries nor keys nor values are given");
+    if ((k || v) && r->kv_rows < r->n) return fail(KF_EINVAL, "kv_rows=%d is below n=%d", r->kv_rows, r->n);
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)r->q_weight | (uintptr_t)r->k_weight) & 15)
+        return fail(KF_EINVAL, "rows and weights must be 16-byte aligned");
+    const int eb = r->dtype == KF_F32 ? 4 : 2;
+    int64_t st[3][2];
+    const int64_t* given[3] = {r->q_stride, r->k_stride, r->v_stride};
+    for (int i = 0; i < 3; ++i) {
+        st[i][0] = given[i][0];
+        st[i][1] = given[i][1];
+        if (st[i][0] == 0 && st[i][1] == 0) {
+            st[i][1] = (i == 0 ? HQ : r->H) * r->d;
+            st[i][0] = st[i][1] * r->n;
+        }
+        if (st[i][0] < 0 || st[i][1] < 0) return fail(KF_EINVAL, "strides must not be negative");
+        if ((st[i][0] * eb) % 16 || (st[i][1] * eb) % 16) return fail(KF_EINVAL, "strides must be multiples of 16 bytes");
+    }
+    if ((r->q_weight || r->k_weight) && (!(r->eps >= 0.0f) || !isfinite(r->eps))) return fail(KF_EINVAL, "eps must be finite and not negative");
+    if (r->rotate != KF_ROTATE_NONE && r->rotate != KF_ROTATE_PAIRS && r->rotate != KF_ROTATE_HALVES)
+        return fail(KF_EINVAL, "unknown rotation %d", r->rotate);
+    if (r->rotate != KF_ROTATE_NONE) {
+        if (!r->inv_freq) return fail(KF_EINVAL, "a rotation needs inv_freq");
+        if (r->rot_dim < 2 || r->rot_dim > r->d || r->rot_dim % 2)
+            return fail(KF_EINVAL, "rot_dim=%d is not an even number in [2, d=%d]", r->rot_dim, r->d);
+        if (r->pos0 < 0) return fail(KF_EINVAL, "pos0 must be non-negative");
+    }
+    kf::RowsArgs a;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.qw = r->q_weight;
+    a.kw = r->k_weight;
+    a.freq = r->inv_freq;
+    a.seq_pos = r->seq_pos;
+    a.seq_n = r->seq_n;
+    a.q_sb = st[0][0];
+    a.q_st = st[0][1];
+    a.k_sb = st[1][0];
+    a.k_st = st[1][1];
+    a.v_sb = st[2][0];
+    a.v_st = st[2][1];
+    a.B = r->B;
+    a.n = r->n;
+    a.kv_rows = r->kv_rows;
+    a.nq = q ? (int32_t)HQ : 0;
+    a.nk = k ? r->H : 0;
+    a.nv = v ? r->H : 0;
+    a.half = r->rotate == KF_ROTATE_NONE ? 0 : r->rot_dim / 2;
+    a.pairs = r->rotate == KF_ROTATE_PAIRS;
+    a.pos0 = r->pos0;
+    a.eps = r->eps;
+    const int64_t blocks = kf::plan_rows(&a);
+    if (blocks > kMaxGrid) return fail(KF_EUNSUPPORTED, "%d sequences of %d tokens exceed the largest launch", r->B, r->n);
+    const hipError_t e = kf::launch_rows(a, blocks, r->d, r->dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(KF_EDEVICE, "rows launch: %s", hipGetErrorString(e));
+    g_err[0] = 0;
+    return KF_OK;
+}
+
+// Workspace of a beam selection: the slices' statistics, then their lists.
+static kf_status check_beams(const kf_beams* b, kf::BeamPlan* p, size_t* stats, size_t* bytes) {
+    if (!b) return fail(KF_EINVAL, "beams description is NULL");
+    if (b->R < 1 || b->W < 1 || b->V < 1) return fail(KF_EINVAL, "sizes must be positive (R=%d W=%d V=%d)", b->R, b->W, b->V);
+    if (b->dtype != KF_F32 && b->dtype != KF_BF16 && b->dtype != KF_F16) return fail(KF_EINVAL, "unknown dtype %d", b->dtype);
+    if (b->W > kf::kBeamMaxW) return fail(KF_EUNSUPPORTED, "%d beams of a request are not built (at most %d)", b->W, kf::kBeamMaxW);
+    if (b->V > 500000) return fail(KF_EUNSUPPORTED, "a vocabulary of %d words is not built (at most 500000)", b->V);
+    const int64_t rows = (int64_t)b->R * b->W;
+    if (rows > 0x7fffffff) return fail(KF_EINVAL, "too many rows");
+    *p = kf::plan_beam(rows, b->W, b->V, b->dtype);
+    if (p->S > kf::kWave) return fail(KF_EUNSUPPORTED, "internal: %d slices of a row", p->S);
+    if (rows * p->S > kMaxGrid) return fail(KF_EUNSUPPORTED, "%lld rows of %d words exceed the largest launch", (long long)rows, b->V);
+    *stats = align_up((size_t)rows * p->S * sizeof(double2), 256);
+    *bytes = *stats + align_up((size_t)rows * p->S * b->W * 8, 256);
+    return KF_OK;
+}
+
+size_t kf_beam_workspace_bytes(const kf_beams* b) {
+    kf::BeamPlan p;
+    size_t stats, bytes;
+    return check_beams(b, &p, &stats, &bytes) == KF_OK ? bytes : 0;
+}
+
+kf_status kf_beam_select(const kf_beams* b, const void* logits, const float* score, const int32_t* done, int32_t* parent,
+                         int32_t* token, float* new_score, int32_t* new_done, int32_t* rank, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    kf::BeamPlan p;
+    size_t stats, bytes;
+    const kf_status st = check_beams(b, &p, &stats, &bytes);
+    if (st != KF_OK) return st;
+    if (!logits || !score || !parent || !token || !new_score)
+        return fail(KF_EINVAL, "logits, score, parent, token and new_score must not be NULL");
+    if ((uintptr_t)logits % (b->dtype == KF_F32 ? 4 : 2)) return fail(KF_EINVAL, "logits must be aligned to their elements");
+    if (b->row_stride != 0 && b->row_stride < b->V) return fail(KF_EINVAL, "row_stride %lld is below V=%d", (long long)b->row_stride, b->V);
+    if ((done || new_done) && (b->eos < 0 || b->eos >= b->V)) return fail(KF_EINVAL, "eos %d outside [0, V=%d)", b->eos, b->V);
+    const kf_status ws = check_ws(workspace, workspace_bytes, bytes);
+    if (ws != KF_OK) return ws;
+    kf::BeamArgs a;
+    a.logits = logits;
+    a.score = score;
+    a.done = done;
+    a.parent = parent;
+    a.token = token;
+    a.new_score = new_score;
+    a.new_done = new_done;
+    a.rank = rank;
+    a.ws_stat = (double2*)workspace;
+    a.ws_list = (unsigned long long*)((char*)workspace + stats);
+    a.row_stride = b->row_stride ? b->row_stride : b->V;
+    a.W = b->W;
+    a.V = b->V;
+    a.S = p.S;
+    a.eos = b->eos;
+    const hipError_t e = kf::launch_beam(a, b->R, b->dtype, p, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(KF_EDEVICE, "beam launch: %s", hipGetErrorString(e));
+    g_err[0] = 0;
+    return KF_OK;
+}
+
 }  // extern "C"

@@ -244,4 +244,54 @@ constexpr int32_t kStripMaxRows = 2048;
 int32_t plan_strips(int64_t U, int32_t n, int32_t d, int32_t dtype, bool bias);
 hipError_t launch_strips(const PrefillArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
 
+// ------------------------------------------------------------------ rows of a projection (kf_rows.hip)
+struct RowsArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    void* Q;
+    void* K;
+    void* V;
+    const void* qw;       // [d] norm weights, or NULL: no norm
+    const void* kw;
+    const float* freq;    // [half]
+    const int32_t* seq_pos;  // [B] position of a sequence's first row, or NULL: pos0
+    const int32_t* seq_n;    // [B] rows of a sequence, or NULL: n
+    int64_t q_sb, q_st, k_sb, k_st, v_sb, v_st;  // elements between sequences, between tokens
+    int32_t B, n, kv_rows;
+    int32_t nq, nk, nv;   // heads of each kind that are asked for
+    int32_t half;         // pairs that are rotated
+    int32_t pairs;        // neighbouring elements (else i and i + half)
+    int32_t pos0;
+    float eps;
+    int32_t tt_shift, tiles;  // log2 of the tokens of a workgroup, tiles of a sequence
+    int32_t hc, chunks;       // heads of a workgroup, workgroups of a tile
+};
+int64_t plan_rows(RowsArgs* a);  // fills the last four; workgroups of the launch
+hipError_t launch_rows(const RowsArgs& a, int64_t blocks, int32_t d, int32_t dtype, hipStream_t stream);
+
+// ------------------------------------------------------------------ beam selection (kf_beam.hip)
+constexpr int32_t kBeamMaxW = 32;
+constexpr size_t kBeamListLds = 48 * 1024;  // of the lists that a request's workgroup joins at a time
+struct BeamArgs {
+    const void* logits;
+    const float* score;
+    const int32_t* done;
+    int32_t* parent;
+    int32_t* token;
+    float* new_score;
+    int32_t* new_done;
+    int32_t* rank;
+    double2* ws_stat;               // [rows][S] largest logit of a slice, sum of its exponentials
+    unsigned long long* ws_list;    // [rows][S][W] its best
+    int64_t row_stride;
+    int32_t W, V, S, eos;
+};
+struct BeamPlan {
+    int32_t NL, S, waves;  // 16-byte loads per lane of a slice, slices per row, waves of a request's workgroup
+    size_t lds_slice, lds_request;
+};
+BeamPlan plan_beam(int64_t rows, int32_t W, int32_t V, int32_t dtype);
+hipError_t launch_beam(const BeamArgs& a, int32_t R, int32_t dtype, const BeamPlan& p, hipStream_t stream);
+
 }  // namespace kf
