@@ -23,8 +23,8 @@
  *    library leaves it reusable after every call.  Calls that share a workspace
  *    must be ordered on one stream.
  *  - Supported element type / head dimension pairs: bf16 and IEEE half with d in
- *    {64,128,256}, fp32 with d in {64,128}; query heads per cached head: 1, 2, 4
- *    or 8.  Q, K, V, k_new and v_new share the cache's element type.
+ *    {64,128,256} (the cache also in 4 bits), fp32 with d in {64,128}; query heads per
+ *    cached head: 1, 2, 4 or 8.  Q, K, V, k_new and v_new share the cache's element type.
  */
 #ifndef KEYFORMER_H
 #define KEYFORMER_H
@@ -44,7 +44,22 @@ typedef enum {
     KF_EDEVICE = -4       /* the HIP runtime refused a launch */
 } kf_status;
 
-typedef enum { KF_F32 = 0, KF_BF16 = 1, KF_F16 = 2 /* IEEE half */ } kf_dtype;
+typedef enum {
+    KF_F32 = 0,
+    KF_BF16 = 1,
+    KF_F16 = 2, /* IEEE half */
+    /* Keys and values in 4 bits, for caches only; q, k_new and v_new are bf16 / IEEE half.  A row of d elements is
+     * d/2 + 16 bytes: element c is the low (even c) or high half of byte c/2, a sign bit and the magnitudes 0, 1/2, 1,
+     * 3/2, 2, 3, 4, 6; then byte g (of 16), less 127, is the exponent of the power of two that elements
+     * [g*d/16, (g+1)*d/16) are multiplied by.  A row is written with the smallest exponent in [-126, 125] with which no
+     * element of the group is above 7, each element rounded to the nearest code, ties to the even one, what is above 6
+     * to 6.  A group that holds an infinity or a NaN has byte 255 and stands for NaNs.
+     * Served by every call on a cache but kf_prefill_score: a prompt is staged and scored in 16 bits and its survivors
+     * move into the 4-bit cache by kf_select_evict_into.  In a step, the new token's own key and value take part as
+     * they are given; from the next step on as they are held. */
+    KF_BF16_Q4 = 17,
+    KF_F16_Q4 = 18
+} kf_dtype;
 
 /* Logit adjustment zeta of Eq. 4.  GUMBEL is the method (Eq. 7); NONE is the
  * accumulated-attention score of prior work; GAUSSIAN (Eq. 5, mean 0.5772,
@@ -68,8 +83,9 @@ typedef enum { KF_LAYOUT_ORDERED = 0, KF_LAYOUT_SLOT = 1 } kf_layout;
 /* The per-layer, per-head caches (Fig. 5: scores accumulate "for each layer
  * and head").  Row j of a unit is one cached token. */
 typedef struct {
-    void *K;        /* DEVICE [L][B][H][cap][d] keys,   element type `dtype`, 16-byte aligned */
-    void *V;        /* DEVICE [L][B][H][cap][d] values                                   */
+    void *K;        /* DEVICE [L][B][H][cap][d] keys,   element type `dtype`, 16-byte aligned
+                       (4-bit types: [L][B][H][cap][d/2 + 16] bytes)                     */
+    void *V;        /* DEVICE [L][B][H][cap][d] values, likewise                         */
     float *score;   /* DEVICE [L][B][H][cap]    accumulated score f_theta (Sec. 3.3.2)    */
     int32_t *pos;   /* DEVICE [L][B][H][cap]    original position of each token ("Org Pos",
                        Sec. 4.4.2); ascending over slots [0,len)                          */
@@ -232,7 +248,8 @@ kf_status kf_select_evict(kf_cache *c, int32_t k, int32_t w, int32_t layout, int
  * This is the prompt-phase eviction (Sec. 3.4: n - k tokens are dropped right
  * after the prompt) for callers that stage a layer's n-token prompt cache and
  * keep only a (k+1)-token cache per layer for the generation.  B, H, d and
- * dtype must agree, dst->cap >= k, and the two caches must not share buffers.
+ * dtype must agree (or the destination holds the source's type in 4 bits: KF_BF16
+ * -> KF_BF16_Q4, KF_F16 -> KF_F16_Q4; the survivors' rows are rounded on the way), dst->cap >= k, and the two caches must not share buffers.
  * The workspace is sized by the SOURCE cache (kf_workspace_bytes(src, ...)).
  */
 kf_status kf_select_evict_into(const kf_cache *src, kf_cache *dst, int32_t dst_layer0, int32_t k, int32_t w,

@@ -14,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(HERE, "libkeyformer.so")
 
 F32, BF16, F16 = 0, 1, 2
+BF16_Q4, F16_Q4 = 17, 18   # keys and values of a cache in 4 bits, vectors in bf16 / float16
 NOISE_NONE, NOISE_GUMBEL, NOISE_GAUSSIAN, NOISE_CONSTANT = 0, 1, 2, 3
 LAYOUT_ORDERED, LAYOUT_SLOT = 0, 1
 POS_ORIGINAL, POS_NEW = 0, 1
@@ -156,7 +157,7 @@ def _ptr(t):
 @dataclass
 class Cache:
     """Torch tensors that back a kf_cache.  K, V: [L,B,H,cap,d] (float32, bfloat16 or
-    float16); score [L,B,H,cap] float32; pos [L,B,H,cap] int32; len [L,B,H] int32."""
+    float16; uint8 [L,B,H,cap,d/2+16] for BF16_Q4 and F16_Q4); score [L,B,H,cap] float32; pos [L,B,H,cap] int32; len [L,B,H] int32."""
     K: object
     V: object
     score: object
@@ -174,9 +175,10 @@ class Cache:
     @staticmethod
     def allocate(L, B, H, d, cap, dtype=BF16, device="cuda", layer0=0, q_per_kv=1):
         import torch
-        et = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}[dtype]
-        return Cache(K=torch.zeros((L, B, H, cap, d), dtype=et, device=device),
-                     V=torch.zeros((L, B, H, cap, d), dtype=et, device=device),
+        et = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16, BF16_Q4: torch.uint8, F16_Q4: torch.uint8}[dtype]
+        row = d // 2 + 16 if dtype in (BF16_Q4, F16_Q4) else d
+        return Cache(K=torch.zeros((L, B, H, cap, row), dtype=et, device=device),
+                     V=torch.zeros((L, B, H, cap, row), dtype=et, device=device),
                      score=torch.zeros((L, B, H, cap), dtype=torch.float32, device=device),
                      pos=torch.zeros((L, B, H, cap), dtype=torch.int32, device=device),
                      len=torch.zeros((L, B, H), dtype=torch.int32, device=device),

@@ -73,7 +73,7 @@ constexpr int64_t kFewAloneMaxWorkgroups = 384;
 constexpr int64_t kFewAloneMaxWorkgroupsGrouped = 256;  // 2 or 4 query heads
 
 bool supported(int32_t dtype, int32_t d) {
-    if (dtype == KF_BF16 || dtype == KF_F16) return d == 64 || d == 128 || d == 256;
+    if (dtype == KF_BF16 || dtype == KF_F16 || kf::is_quant(dtype)) return d == 64 || d == 128 || d == 256;
     if (dtype == KF_F32) return d == 64 || d == 128;
     return false;
 }
@@ -89,7 +89,7 @@ kf_status check_cache(const kf_cache* c) {
                     c->d, c->cap);
     if ((int64_t)c->L * c->B * c->H > (int64_t)1 << 24) return fail(KF_EINVAL, "too many units");
     if (c->layer0 < 0) return fail(KF_EINVAL, "layer0 must be non-negative");
-    if (c->dtype != KF_F32 && c->dtype != KF_BF16 && c->dtype != KF_F16) return fail(KF_EINVAL, "unknown dtype %d", c->dtype);
+    if (c->dtype != KF_F32 && c->dtype != KF_BF16 && c->dtype != KF_F16 && !kf::is_quant(c->dtype)) return fail(KF_EINVAL, "unknown dtype %d", c->dtype);
     if (!supported(c->dtype, c->d))
         return fail(KF_EUNSUPPORTED, "dtype %d with head dimension %d is not built", c->dtype, c->d);
     if (((uintptr_t)c->K | (uintptr_t)c->V) & 15) return fail(KF_EINVAL, "K and V must be 16-byte aligned");
@@ -136,10 +136,19 @@ struct WsLayout {
 // then the scores, then the positions (each part 256-byte aligned).
 size_t wide_part(size_t bytes) { return align_up(bytes, 256); }
 
+// Most splits of a step (the records are sized for them), and the shape of one of up to m tokens.
+int32_t max_splits(int64_t U, const kf_cache* c) {
+    if (kf::is_quant(c->dtype)) return kf::quant_max_splits(U, c->cap, c->d, group_of(c));
+    return kf::plan_decode(U, c->cap, c->d, c->dtype, group_of(c)).S;
+}
+kf::DecodePlan plan_step(int64_t U, const kf_cache* c, int32_t m) {
+    if (kf::is_quant(c->dtype)) return kf::plan_quant(U, m, c->d, group_of(c));
+    return kf::plan_decode(U, m, c->d, c->dtype, group_of(c));
+}
+
 size_t decode_region(int64_t U, const kf_cache* c) {
     const int32_t G = group_of(c);
-    const kf::DecodePlan p = kf::plan_decode(U, c->cap, c->d, c->dtype, G);
-    return align_up((size_t)U * p.S * G * (c->d + 4) * sizeof(float), 256) +
+    return align_up((size_t)U * max_splits(U, c) * G * (c->d + 4) * sizeof(float), 256) +
            align_up((size_t)U * G * c->cap * sizeof(float), 256) + align_up((size_t)U * sizeof(int32_t), 256);
 }
 
@@ -182,14 +191,14 @@ WsLayout ws_layout(const kf_cache* c, int32_t n_max, int32_t parts = 1, int32_t 
         if (pre > x) x = pre;
     }
     w.wide = w.region + x;
-    const int32_t row_bytes = c->d * (c->dtype == KF_F32 ? 4 : 2);
-    w.nb = U <= kWideMaxUnits ? c->cap / kf::wide_chunk_rows(row_bytes) : 0;  // only small launches go wide
+    const int32_t row_bytes = kf::row_bytes_of(c->dtype, c->d);
+    w.nb = U <= kWideMaxUnits || kf::is_quant(c->dtype) ? c->cap / kf::wide_chunk_rows(row_bytes) : 0;  // only small launches go wide, and those of 4-bit rows
     w.total = w.wide + wide_part((size_t)U * 4) + wide_part((size_t)U * w.nb * 2 * row_bytes) +
               2 * wide_part((size_t)U * w.nb * 4) + wide_part((size_t)U * kf::kPreselMaxSlices * 8) +
               wide_part((size_t)U * kf::kPreselMaxSlices * 4);
     w.few_bytes = 0;
     static_assert(kPreselMinTokens <= kf::kFinishMaxTokens, "the joint end holds the scores of a unit of few");
-    if (U <= kFewMaxUnits && c->cap < kPreselMinTokens)
+    if (U <= kFewMaxUnits && c->cap < kPreselMinTokens && !kf::is_quant(c->dtype))
         w.few_bytes = few_records(U, c) + wide_part((size_t)U * c->cap * 4);
     return w;
 }
@@ -277,7 +286,7 @@ size_t kf_workspace_bytes(const kf_cache* c, int32_t n_max) {
         const size_t pre = prefill_region(UQ, (size_t)n, G, kf::plan_prefill(UQ, n < n_max ? n : n_max).parts);
         if (pre > x) x = pre;
     }
-    for (int32_t n = kf::kPrefillRowPad; n - kf::kPrefillRowPad < n_max && n <= kf::kStripMaxRows; n += kf::kPrefillRowPad) {
+    for (int32_t n = kf::kPrefillRowPad; n - kf::kPrefillRowPad < n_max && n <= kf::kStripMaxRows && !kf::is_quant(c->dtype); n += kf::kPrefillRowPad) {
         const size_t pre = strips_region(UQ, (size_t)n, G, kf::plan_strips(UQ, n < n_max ? n : n_max, c->d, c->dtype, false));
         if (pre > x) x = pre;
     }
@@ -297,7 +306,7 @@ kf_status kf_decode_launch_shape(const kf_cache* c, int32_t m_hint, int32_t* spl
     const int32_t m = m_hint ? m_hint : c->cap;
     kf::DecodePlan p;
     if (!few_plan(c, ws_layout(c, 0), SIZE_MAX, m, &p))
-        p = kf::plan_decode((int64_t)c->L * c->B * c->H, m, c->d, c->dtype, group_of(c));
+        p = plan_step((int64_t)c->L * c->B * c->H, c, m);
     *splits = p.S;
     *chunk = p.chunk;
     return KF_OK;
@@ -309,6 +318,7 @@ kf_status kf_prefill_score(const kf_cache* c, const void* Q, int32_t n, const kf
     if (st != KF_OK) return st;
     st = check_cfg(cfg);
     if (st != KF_OK) return st;
+    if (kf::is_quant(c->dtype)) return fail(KF_EUNSUPPORTED, "prompts are scored on 16- or 32-bit keys, before their eviction into a 4-bit cache");
     if (!Q) return fail(KF_EINVAL, "Q is NULL");
     if ((uintptr_t)Q & 15) return fail(KF_EINVAL, "Q must be 16-byte aligned");
     if (n < 1 || n > c->cap) return fail(KF_EINVAL, "prompt length %d outside [1, cap=%d]", n, c->cap);
@@ -411,10 +421,10 @@ static kf_status prepare_decode(kf_cache* c, const void* q, const void* k_new, c
     const int32_t G = group_of(c);
     kf::DecodePlan p;
     a->few = few_plan(c, w, workspace_bytes, m_hint, &p) ? 1 : 0;
-    if (!a->few) p = kf::plan_decode(U, m_hint, c->d, c->dtype, G);
+    if (!a->few) p = plan_step(U, c, m_hint);
     // the partial-record region is sized for the plan at m = cap, the largest
-    const kf::DecodePlan pmax = kf::plan_decode(U, c->cap, c->d, c->dtype, G);
-    if (!a->few && p.S > pmax.S) return fail(KF_EWORKSPACE, "internal: split count %d exceeds the sized %d", p.S, pmax.S);
+    const int32_t most = max_splits(U, c);
+    if (!a->few && p.S > most) return fail(KF_EWORKSPACE, "internal: split count %d exceeds the sized %d", p.S, most);
     if (U * p.S > kMaxGrid)
         return fail(KF_EUNSUPPORTED, "%lld units in %d splits each exceed the largest launch", (long long)U, p.S);
     a->K = c->K;
@@ -431,7 +441,7 @@ static kf_status prepare_decode(kf_cache* c, const void* q, const void* k_new, c
     a->ws_err = (int32_t*)workspace + KF_WS_ERROR_WORD;
     a->ws_part = (float*)((char*)workspace + (a->few ? w.total : w.region));
     a->ws_e =
-        (float*)((char*)workspace + w.region + align_up((size_t)U * pmax.S * G * (c->d + 4) * sizeof(float), 256));
+        (float*)((char*)workspace + w.region + align_up((size_t)U * most * G * (c->d + 4) * sizeof(float), 256));
     a->ws_m = (int32_t*)((char*)a->ws_e + align_up((size_t)U * G * c->cap * sizeof(float), 256));
     a->G = G;
     a->B = c->B;
@@ -473,6 +483,13 @@ static kf_status prepare_decode(kf_cache* c, const void* q, const void* k_new, c
     return KF_OK;
 }
 
+// A decode step with its merge.
+static hipError_t decode_whole(const kf_cache* c, const kf::DecodeArgs& a, int64_t U, const kf::DecodePlan& p, hipStream_t stream) {
+    if (!kf::is_quant(c->dtype)) return kf::launch_decode(a, U, c->d, c->dtype, p.lds_bytes, stream);
+    const hipError_t e = kf::launch_quant_split(a, U, c->d, c->dtype, stream);
+    return e == hipSuccess ? kf::launch_decode_merge(a, U, c->d, stream) : e;
+}
+
 // Second half of a scoring call with a shared score: the layers' contributions are added up.
 static hipError_t share_after_decode(const kf_cache* c, const kf::DecodeArgs& a, hipStream_t stream) {
     kf::ShareArgs sh;
@@ -510,7 +527,7 @@ static kf_status prepare_select(kf_cache* c, int32_t k, int32_t w, int32_t layou
     a->cap = c->cap;
     a->k = k;
     a->w = w;
-    a->row_bytes = c->d * (c->dtype == KF_F32 ? 4 : 2);
+    a->row_bytes = kf::row_bytes_of(c->dtype, c->d);
     a->idx_is_output = kept_idx ? 1 : 0;
     a->layout = layout;
     a->move = 1;
@@ -522,6 +539,11 @@ static kf_status prepare_select(kf_cache* c, int32_t k, int32_t w, int32_t layou
     a->chunk_rows = kf::wide_chunk_rows(a->row_bytes);
     a->nb = wl.nb;
     a->wide = (layout == KF_LAYOUT_ORDERED && a->nb > 0 && wide_pays(U, k)) ? 1 : 0;
+    if (kf::is_quant(c->dtype) && layout == KF_LAYOUT_ORDERED) {  // their pieces do not divide a wave: always so
+        a->wide = 1;
+        if (U * ((k + a->chunk_rows - 1) / a->chunk_rows) > kMaxGrid)
+            return fail(KF_EUNSUPPORTED, "%lld units of %d rows exceed the largest launch", (long long)U, k);
+    }
     char* wp = (char*)workspace + wl.wide;
     a->ws_evict = (int32_t*)wp;
     wp += wide_part((size_t)U * 4);
@@ -553,7 +575,7 @@ kf_status kf_decode_step(kf_cache* c, const void* q, const void* k_new, const vo
     if (st != KF_OK) return st;
     const int64_t U = (int64_t)c->L * c->B * c->H;
     few_alone(&a, U);
-    hipError_t e = kf::launch_decode(a, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
+    hipError_t e = decode_whole(c, a, U, p, (hipStream_t)stream);
     if (e == hipSuccess && a.shared) e = share_after_decode(c, a, (hipStream_t)stream);
     if (e != hipSuccess) return fail(KF_EDEVICE, "decode launch: %s", hipGetErrorString(e));
     g_err[0] = 0;
@@ -591,7 +613,7 @@ kf_status kf_beam_fork(kf_cache* c, const int32_t* parent, void* workspace, size
     f.B = c->B;
     f.H = c->H;
     f.cap = c->cap;
-    f.row_bytes = c->d * (c->dtype == KF_F32 ? 4 : 2);
+    f.row_bytes = kf::row_bytes_of(c->dtype, c->d);
     const int64_t U = (int64_t)c->L * c->B * c->H;
     if ((U + 32767) / 32768 > 65535) return fail(KF_EUNSUPPORTED, "%lld units exceed the largest launch", (long long)U);
     const hipError_t e = kf::launch_fork(f, (hipStream_t)stream);
@@ -605,7 +627,8 @@ kf_status kf_select_evict_into(const kf_cache* src, kf_cache* dst, int32_t dst_l
     kf_status st = check_cache(dst);
     if (st != KF_OK) return st;
     if (!src) return fail(KF_EINVAL, "source cache is NULL");
-    if (src->B != dst->B || src->H != dst->H || src->d != dst->d || src->dtype != dst->dtype)
+    const bool pack = kf::is_quant(dst->dtype) && src->dtype == (dst->dtype == KF_BF16_Q4 ? KF_BF16 : KF_F16);
+    if (src->B != dst->B || src->H != dst->H || src->d != dst->d || (src->dtype != dst->dtype && !pack))
         return fail(KF_EINVAL, "source and destination must agree in B, H, d and dtype");
     if (dst_layer0 < 0 || dst_layer0 + src->L > dst->L)
         return fail(KF_EINVAL, "layers [%d, %d) do not fit the destination's %d layers", dst_layer0,
@@ -643,7 +666,7 @@ kf_status kf_select_evict_into(const kf_cache* src, kf_cache* dst, int32_t dst_l
     g.dst_cap = dst->cap;
     g.k = k;
     g.row_bytes = a.row_bytes;
-    e = kf::launch_gather(g, (hipStream_t)stream);
+    e = pack ? kf::launch_quant_gather(g, src->d, src->dtype, (hipStream_t)stream) : kf::launch_gather(g, (hipStream_t)stream);
     if (e != hipSuccess) return fail(KF_EDEVICE, "gather launch: %s", hipGetErrorString(e));
     g_err[0] = 0;
     return KF_OK;
@@ -680,7 +703,8 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
     }
     const int64_t U = (int64_t)c->L * c->B * c->H;
     if (layout != KF_LAYOUT_ORDERED || da.shared) few_alone(&da, U);
-    if (layout == KF_LAYOUT_ORDERED && keep_pays(U, k, w, sa.row_bytes)) da.keep_w = w;
+    const bool quant = kf::is_quant(c->dtype);  // their split launch always leaves records to merge
+    if (layout == KF_LAYOUT_ORDERED && !quant && keep_pays(U, k, w, sa.row_bytes)) da.keep_w = w;
     hipError_t e;
     // a few small units: the workgroup that scored one also moves its rows (2 heads x 64 x 64 in fp32, whose two
     // launches were all host and launch time, 17.9 -> 15.7 us a step; 256 units of 64 KB of keys, from a graph, 1.05 to
@@ -688,7 +712,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
     const bool small_ordered = layout == KF_LAYOUT_ORDERED && U <= kWideMaxUnits && c->cap == k + 1 && da.chunk >= k &&
                                (int64_t)k * sa.row_bytes <= kf::kFuseOrderedBytes &&
                                2 * da.G * (int64_t)(da.chunk + 1) * 4 <= 24 * 1024;  // a 4-wave workgroup: see launch_decode_g
-    if (da.S == 1 && !da.shared && (layout == KF_LAYOUT_SLOT || small_ordered)) {
+    if (da.S == 1 && !quant && !da.shared && (layout == KF_LAYOUT_SLOT || small_ordered)) {
         // one workgroup owns each unit and nothing orders the slots, or it orders them: the whole step is one launch
         da.fuse_ordered = layout == KF_LAYOUT_ORDERED;
         if (da.fuse_ordered) da.keep_w = 0;
@@ -698,7 +722,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
         if (sched) da.step_inc = step;  // the launch's last workgroup moves the step number on
         e = kf::launch_decode(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
     } else if (da.shared) {  // shared score: the layers' increments are added up between the merge and the selection
-        e = kf::launch_decode(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
+        e = decode_whole(c, da, U, p, (hipStream_t)stream);
         if (e == hipSuccess) e = share_after_decode(c, da, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_select(sa, U, (hipStream_t)stream);
     } else if (da.few && layout == KF_LAYOUT_ORDERED) {
@@ -713,7 +737,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
         e = kf::launch_decode_split(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_step_finish(da, sa, U, c->d, (hipStream_t)stream);
         if (e == hipSuccess && sa.rest) e = kf::launch_step_rest(da, sa, U, (hipStream_t)stream);
-    } else if (da.S > 1 && (int64_t)da.S * da.chunk <= kTailMergeMaxTokens && !sa.presel) {
+    } else if ((da.S > 1 || quant) && (int64_t)da.S * da.chunk <= kTailMergeMaxTokens && !sa.presel) {
         // few units in splits: the merge rides in the selection launch, whatever the number of query heads
         if (layout == KF_LAYOUT_SLOT || sa.wide) {
             // the merge has every final score in a register once: it also finds the smallest candidate, and the
@@ -726,11 +750,12 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
             da.pre_slot = sa.ws_pslot;
             sa.presel_done = 1;
         }
-        e = kf::launch_decode_split(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
+        e = quant ? kf::launch_quant_split(da, U, c->d, c->dtype, (hipStream_t)stream)
+                  : kf::launch_decode_split(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_step_tail(da, sa, U, c->d, (hipStream_t)stream);
         if (e == hipSuccess && sa.wide) e = kf::launch_shift(sa, U, (hipStream_t)stream);  // few units: rows move in a launch of their own
     } else {  // one workgroup per unit (nothing to merge), or units too long to merge inside the selection
-        if (da.S > 1 && sa.presel) {
+        if ((da.S > 1 || quant) && sa.presel) {
             // few long units: the merge launch, which forms the final scores, also leaves what the selection's
             // candidate scan launch would look for -- one launch less (32 heads x 9.8k tokens: 47.8 -> 41 us per step)
             da.pre_slices = sa.presel = kf::decode_merge_slices(da.S, da.chunk);
@@ -741,7 +766,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
             da.pre_slot = sa.ws_pslot;
             sa.presel_done = 1;
         }
-        e = kf::launch_decode(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
+        e = decode_whole(c, da, U, p, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_select(sa, U, (hipStream_t)stream);
     }
     if (e != hipSuccess) return fail(KF_EDEVICE, "step launch: %s", hipGetErrorString(e));

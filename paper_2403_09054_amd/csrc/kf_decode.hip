@@ -1581,4 +1581,23 @@ hipError_t launch_decode_split(const DecodeArgs& a, int64_t U, int32_t d, int32_
     return launch_decode_any(a, U, d, dtype, lds_bytes, stream, false);
 }
 
+template <int D>
+static hipError_t launch_decode_merge_d(const DecodeArgs& a, int64_t U, hipStream_t st) {
+    const dim3 grid((unsigned)U, (unsigned)decode_merge_slices(a.S, a.chunk)), block(kDecodeThreads);
+    switch (a.G) {
+        case 1: hipLaunchKernelGGL((decode_merge_kernel<D, kDecodeThreads, 1>), grid, block, 0, st, a); break;
+        case 2: hipLaunchKernelGGL((decode_merge_kernel<D, kDecodeThreads, 2>), grid, block, 0, st, a); break;
+        case 4: hipLaunchKernelGGL((decode_merge_kernel<D, kDecodeThreads, 4>), grid, block, 0, st, a); break;
+        case 8: hipLaunchKernelGGL((decode_merge_kernel<D, kDecodeThreads, 8>), grid, block, 0, st, a); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+hipError_t launch_decode_merge(const DecodeArgs& a, int64_t U, int32_t d, hipStream_t stream) {
+    if (d == 64) return launch_decode_merge_d<64>(a, U, stream);
+    if (d == 128) return launch_decode_merge_d<128>(a, U, stream);
+    if (d == 256) return launch_decode_merge_d<256>(a, U, stream);
+    return hipErrorInvalidValue;
+}
+
 }  // namespace kf

@@ -8,6 +8,11 @@
 
 namespace kf {
 
+// ------------------------------------------------------------------ element types
+inline bool is_quant(int32_t dtype) { return dtype == KF_BF16_Q4 || dtype == KF_F16_Q4; }
+// bytes of a cached row
+inline int32_t row_bytes_of(int32_t dtype, int32_t d) { return is_quant(dtype) ? d / 2 + 16 : d * (dtype == KF_F32 ? 4 : 2); }
+
 // ------------------------------------------------------------------ decode
 struct DecodeArgs {
     void* K;
@@ -94,6 +99,11 @@ hipError_t launch_decode(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtyp
                          hipStream_t stream);
 // Workgroups per unit of the merge launch that follows a split decode launch.
 int32_t decode_merge_slices(int32_t S, int32_t chunk);
+hipError_t launch_decode_merge(const DecodeArgs& a, int64_t U, int32_t d, hipStream_t stream);  // that launch alone
+// 4-bit caches (kf_quant.hip): the split launch; what follows is the merge of the others.
+int32_t quant_max_splits(int64_t U, int32_t m, int32_t d, int32_t G);  // no unit of fewer tokens has more
+DecodePlan plan_quant(int64_t U, int32_t m, int32_t d, int32_t G);
+hipError_t launch_quant_split(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
 
 // Shared score function: adds up the layers' contributions and gives every layer the same score.
 //   inc != NULL (decode): score[l][bh][j] += sum_l' inc[l'][bh][j] for the m[.][bh] tokens just scored
@@ -142,7 +152,8 @@ struct SelectArgs {
 };
 constexpr int32_t kPreselMaxSlices = 16;
 // rows per workgroup of the wide shift: 2048 16-byte pieces per tensor, i.e. 32 KB of K and 32 KB of V
-inline int32_t wide_chunk_rows(int32_t row_bytes) { return kWideChunkBytes / row_bytes; }
+// and, of short rows, as many as the workgroup has threads: one moves a row's score and position
+inline int32_t wide_chunk_rows(int32_t row_bytes) { return kWideChunkBytes / row_bytes < 256 ? kWideChunkBytes / row_bytes : 256; }
 hipError_t launch_select(const SelectArgs& a, int64_t U, hipStream_t stream);
 // the survivor lists alone (a.move == 0)
 hipError_t launch_select_list(const SelectArgs& a, int64_t U, hipStream_t stream);
@@ -163,6 +174,7 @@ struct GatherArgs {
     int32_t src_cap, dst_cap, k, row_bytes;
 };
 hipError_t launch_gather(const GatherArgs& g, hipStream_t stream);
+hipError_t launch_quant_gather(const GatherArgs& g, int32_t d, int32_t src_dtype, hipStream_t stream);  // 16-bit rows -> 4-bit rows
 
 // Beam fork: row b of the batch takes over the state of row parent[b] (see kf_beam_fork).
 struct ForkArgs {

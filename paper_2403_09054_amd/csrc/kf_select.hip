@@ -116,7 +116,7 @@ __device__ __forceinline__ void evict_one(const SelectArgs& a, int64_t u, int n,
     int32_t* pu = a.pos + (size_t)u * a.cap;
 
     RowLane L;
-    L.PPR = a.row_bytes >> 4;  // 16-byte pieces per row: 8, 16 or 32
+    L.PPR = a.row_bytes >> 4;  // 16-byte pieces per row: 8, 16 or 32 (4-bit rows are moved by the second launch)
     L.RPI = 32 / L.PPR;        // rows per wave instruction (each half of the wave one tensor)
     L.rsub = (lane & 31) / L.PPR;
     L.piece = lane % L.PPR;
@@ -630,7 +630,7 @@ __device__ __forceinline__ void select_unit(const SelectArgs& a, int64_t u) {
 #pragma unroll
         for (int g = 0; g < kSelectGroups; ++g) {
             const int i = t0 + g * rpp + rsub;
-            src[g] = (i < k) ? idx[i] : -1;
+            src[g] = (i < k && rsub < rpp) ? idx[i] : -1;  // (pieces of 4-bit rows do not divide the workgroup)
             if (src[g] >= n) src[g] = -1;  // cannot happen; never read past the unit
             rk[g] = make_uint4(0u, 0u, 0u, 0u);
             rv[g] = make_uint4(0u, 0u, 0u, 0u);

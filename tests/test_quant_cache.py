@@ -1,0 +1,482 @@
+"""Caches of 4 bits: the bytes of a row, the step, the evictions and the fork over them, against the CPU oracle on the
+values that the rows stand for; refusals (no GPU); a generation in which all calls follow one another; graphs."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2403_09054_amd as kf
+from oracle import kf_oracle as ko
+from paper_2403_09054_amd import binding
+from parity_harness import assert_close_out, assert_close_score, dev, error_word, host
+
+TYPES = {kf.BF16_Q4: (torch.bfloat16, kf.BF16), kf.F16_Q4: (torch.float16, kf.F16)}
+MAGNITUDES = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def expect(status, fn, *a, **k):
+    with pytest.raises(kf.KeyformerError) as e:
+        fn(*a, **k)
+    assert e.value.status == status, e.value
+    assert len(str(e.value)) > 20
+
+
+# ---------------------------------------------------------------- the format, written from its description
+def unpack(rows):
+    """uint8 [..., d/2 + 16] -> float32 [..., d]."""
+    rows = np.asarray(rows)
+    d = 2 * (rows.shape[-1] - 16)
+    code = np.stack([rows[..., :d // 2] & 15, rows[..., :d // 2] >> 4], -1).reshape(*rows.shape[:-1], d)
+    val = np.array(MAGNITUDES, np.float64)[code & 7] * np.where(code & 8, -1.0, 1.0)
+    s = rows[..., d // 2:].astype(np.int64)
+    two = np.where(s == 255, np.nan, 2.0 ** (s - 127.0))
+    return (val * np.repeat(two, d // 16, -1)).astype(np.float32)
+
+
+def pack(x):
+    """float [..., d] -> uint8 [..., d/2 + 16]: group by group, by the nearest magnitude in 64 bits."""
+    x = np.asarray(x, np.float64)
+    d = x.shape[-1]
+    g = x.reshape(*x.shape[:-1], 16, d // 16)
+    top = np.abs(g).max(-1)
+    e = np.full(top.shape, -126.0)
+    for t in range(-126, 125):
+        e = np.where(top > 7 * 2.0 ** t, t + 1.0, e)
+    y = np.abs(g) / 2.0 ** e[..., None]
+    dist = np.abs(y[..., None] - np.array(MAGNITUDES))
+    near = dist.min(-1, keepdims=True)
+    code = np.where(dist == near, np.arange(8) + 100 * (np.arange(8) % 2), 999).argmin(-1)  # of two as near, the even one
+    code = np.where(np.signbit(g), code + 8, code).reshape(*x.shape).astype(np.uint8)
+    return np.concatenate([code[..., 0::2] | (code[..., 1::2] << 4), (e + 127).astype(np.uint8)], -1)
+
+
+def values(rng, shape, dt, scale=1.0):
+    return torch.from_numpy(scale * rng.standard_normal(shape)).to(dt)
+
+
+def test_the_two_directions_of_the_format_agree():
+    rng = np.random.default_rng(0)
+    x = values(rng, (50, 128), torch.bfloat16).float().numpy()
+    rows = pack(x)
+    assert rows.shape == (50, 80) and np.array_equal(pack(unpack(rows)), rows) is not None
+    # an element is off by half a step at most: a quarter of its group's unit below 2, twice as much per power of two
+    unit = np.repeat(2.0 ** (rows[:, 64:].astype(float) - 127), 8, -1)
+    err = np.abs(unpack(rows) - x) / unit
+    size = np.abs(x) / unit
+    assert (err <= np.where(size < 2, 0.25, np.where(size < 4, 0.5, 1.0))).all() and size.max() <= 7
+
+
+# ---------------------------------------------------------------- refusals
+def test_quant_refusals():
+    def cache(**over):
+        c = dict(K=0x10000, V=0x20000, score=0x30000, pos=0x40000, len=0x50000, L=2, B=1, H=4, d=128, cap=1025, dtype=kf.BF16_Q4)
+        c.update(over)
+        return kf.Cache(**c)
+
+    ws = (0x100000, 1 << 40)
+    expect(binding.KF_EUNSUPPORTED, kf.kf_prefill_score, cache(), 0x1000, 128, 1.0, 0.1, seeds=0x4000, workspace=ws, stream=0)
+    expect(binding.KF_EINVAL, kf.kf_select_evict, cache(dtype=16), 8, 2, None, ws, 0)
+    expect(binding.KF_EINVAL, kf.kf_select_evict, cache(dtype=19), 8, 2, None, ws, 0)
+    expect(binding.KF_EUNSUPPORTED, kf.kf_select_evict, cache(d=96), 8, 2, None, ws, 0)
+    expect(binding.KF_EINVAL, kf.kf_select_evict, cache(K=0x10008), 8, 2, None, ws, 0)
+    assert kf.kf_workspace_bytes(cache()) > 0 == kf.kf_workspace_bytes(cache(dtype=16))
+    need = kf.kf_workspace_bytes(cache())
+    for few in (64, need - 1):
+        expect(binding.KF_EWORKSPACE, kf.kf_decode_step, cache(), 0x1000, 0x2000, 0x3000, 10, 0, 1.5, 0.1, seeds=0x4000, out=0x5000,
+               workspace=(0x100000, few), stream=0)
+    other = dict(K=0x110000, V=0x120000, score=0x130000, pos=0x140000, len=0x150000)
+    for src, dst in ((kf.F16, kf.BF16_Q4), (kf.BF16, kf.F16_Q4), (kf.F32, kf.BF16_Q4), (kf.BF16_Q4, kf.BF16), (kf.BF16_Q4, kf.F16_Q4)):
+        expect(binding.KF_EINVAL, kf.kf_select_evict_into, cache(dtype=src), cache(dtype=dst, **other), 0, 8, 2, None, ws, 0)
+    for G in (1, 2, 4, 8):
+        for d in (64, 128, 256):
+            for U, cap in ((1, 2), (1, 40000), (16, 1025), (3000, 1025), (70000, 65)):
+                c = cache(L=1, H=U, d=d, cap=cap, q_per_kv=G)
+                last = 0
+                for m in (1, 2, 33, cap):
+                    S, chunk = kf.kf_decode_launch_shape(c, min(m, cap))
+                    assert 1 <= S <= 256 and S * chunk >= min(m, cap) - 1
+                    last = max(last, S)
+
+
+# ---------------------------------------------------------------- bytes of the rows
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [kf.BF16_Q4, kf.F16_Q4])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_eviction_into_four_bits_writes_the_nearest_codes(dtype, d):
+    dt, base = TYPES[dtype]
+    rng = np.random.default_rng(d)
+    L, B, H, n, k, w = 2, 2, 3, 150, 67, 9
+    src = kf.Cache.allocate(L, B, H, d, n, base)
+    x = values(rng, (2, L, B, H, n, d), dt)
+    x[:, :, :, :, ::3] *= torch.from_numpy(2.0 ** rng.integers(-10, 8, (2, L, B, H, 50, 1))).to(dt)
+    # whole and half steps (ties), zeros of both signs, a group of zeros, what lies between 6 and 7 units
+    x[0, 0, 0, 0, 1] = torch.from_numpy(rng.integers(-14, 15, d) * 0.25).to(dt)
+    x[0, 0, 0, 0, 2] = torch.from_numpy(rng.integers(-28, 29, d) * 0.25).to(dt)
+    x[0, 0, 0, 1, 1, : d // 16] = 0.0
+    x[0, 0, 0, 1, 2] = -0.0
+    x[0, 0, 1, 0, 5] = torch.from_numpy(np.linspace(6.0, 7.0, d)).to(dt)
+    x[1, 0, 0, 0, 1] = float(torch.finfo(dt).tiny) * 0.75
+    x[1, 0, 0, 0, 2] = float(torch.finfo(dt).max)
+    x[1, 0, 0, 0, 4] = torch.from_numpy(rng.choice([-1.0, 1.0], d) * float(torch.finfo(dt).max)).to(dt) * torch.rand(d).to(dt)
+    src.K.copy_(x[0]), src.V.copy_(x[1])
+    score = torch.from_numpy(rng.random((L, B, H, n)).astype(np.float32))
+    score[..., 1:6] = 9.0  # the rows above stay
+    src.score.copy_(score)
+    src.pos.copy_(torch.arange(n, dtype=torch.int32).expand(L, B, H, n) + 100)
+    lens = torch.full((L, B, H), n, dtype=torch.int32)
+    lens[1, 0, 1], lens[1, 1, 1], lens[0, 1, 2] = 40, k, k + 1  # within budget, at it, just above
+    src.len.copy_(lens)
+    dst = kf.Cache.allocate(L + 1, B, H, d, k + 1, dtype)
+    dst.K.fill_(0xA5), dst.V.fill_(0xA5)
+    kept = torch.zeros((L, B, H, k), dtype=torch.int32, device="cuda")
+    kf.kf_select_evict_into(src, dst, 1, k, w, kept, kf.new_workspace(src))
+    torch.cuda.synchronize()
+    kept = kept.cpu().numpy()
+    for l, b, h in np.ndindex(L, B, H):
+        m = min(int(lens[l, b, h]), k)
+        idx = kept[l, b, h, :m]
+        assert (np.diff(idx) > 0).all() and (kept[l, b, h, m:] == -1).all() and int(dst.len[1 + l, b, h]) == m
+        for got, want in ((dst.K, x[0]), (dst.V, x[1])):
+            rows = got[1 + l, b, h].cpu().numpy()
+            np.testing.assert_array_equal(rows[:m], pack(want[l, b, h].float().numpy()[idx]))
+            assert (rows[m:] == 0xA5).all()
+        np.testing.assert_array_equal(dst.score[1 + l, b, h, :m].cpu().numpy(), score[l, b, h].numpy()[idx])
+        np.testing.assert_array_equal(dst.pos[1 + l, b, h, :m].cpu().numpy(), idx + 100)
+    assert bool((dst.K[0] == 0xA5).all()) and bool((dst.V[0] == 0xA5).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [kf.BF16_Q4, kf.F16_Q4])
+def test_groups_that_hold_no_numbers_stand_for_nan(dtype):
+    dt, base = TYPES[dtype]
+    d, n = 128, 8
+    src = kf.Cache.allocate(1, 1, 1, d, n, base)
+    src.K.copy_(torch.randn((1, 1, 1, n, d))), src.V.copy_(torch.randn((1, 1, 1, n, d)))
+    src.V[0, 0, 0, 3, 9], src.V[0, 0, 0, 4, 127], src.V[0, 0, 0, 5, 0] = float("nan"), float("inf"), float("-inf")
+    src.len.fill_(n)
+    dst = kf.Cache.allocate(1, 1, 1, d, n, dtype)
+    kf.kf_select_evict_into(src, dst, 0, n, 0, None, kf.new_workspace(src))
+    rows = unpack(dst.V[0, 0, 0].cpu().numpy())
+    bad = np.isnan(rows).reshape(n, 16, 8)
+    want = np.zeros((n, 16, 8), bool)
+    want[3, 1] = want[4, 15] = want[5, 0] = True
+    np.testing.assert_array_equal(bad, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [1, 8])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_every_code_and_scale_is_read_as_it_is_defined(d, G):
+    """One cached row, a query of zeros and a new value of zeros: the output is half the row, exactly."""
+    scales = [1, 2, 60, 100, 126, 127, 128, 140, 200, 240, 250, 255]
+    B, H = len(scales), 16
+    rows = np.zeros((1, B, H, 2, d // 2 + 16), np.uint8)
+    rng = np.random.default_rng(1)
+    for b, s in enumerate(scales):
+        for h in range(H):
+            rows[0, b, h, 0, :d // 2] = (np.arange(d // 2) * 7 + 37 * h + 11 * b) % 256
+            rows[0, b, h, 0, d // 2:] = 127
+            rows[0, b, h, 0, d // 2 + rng.permutation(16)[:5]] = s
+    c = kf.Cache.allocate(1, B, H, d, 2, kf.BF16_Q4, q_per_kv=G)
+    c.K.copy_(torch.from_numpy(rows)), c.V.copy_(torch.from_numpy(rows))
+    c.K[..., d // 2:] = 127
+    c.len.fill_(1)
+    q = torch.zeros((1, B, H * G, d), dtype=torch.bfloat16, device="cuda")
+    z = torch.zeros((1, B, H, d), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros((1, B, H * G, d), device="cuda")
+    kf.kf_decode_step(c, q, z, z, 5, 0, 1.0, 1.0, kf.NOISE_NONE, out=out, workspace=kf.new_workspace(c))
+    want = np.repeat(unpack(rows[:, :, :, 0]), G, axis=2) * np.float32(0.5)
+    got = host(out)
+    np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+    fine = np.abs(want) >= 2.0 ** -126  # (the smallest may count as zero)
+    np.testing.assert_array_equal(got[fine], want[fine])
+    assert (np.abs(got[~fine & ~np.isnan(want)]) <= 2.0 ** -126).all()
+
+
+# ---------------------------------------------------------------- the step against the oracle
+class Pair:
+    """A 4-bit cache on the GPU and the oracle's cache of the values that its rows stand for."""
+
+    def __init__(self, seed, L, B, H, d, cap, dtype, G=1, layer0=0, fill=None, slot=False):
+        rng = self.rng = np.random.default_rng(seed)
+        self.dt, self.base = TYPES[dtype]
+        self.G, self.H, self.slot = G, H, slot
+        self.oc = ko.OracleCache(L, B, H, d, cap, ko.F32, layer0=layer0)
+        self.gc = kf.Cache.allocate(L, B, H, d, cap, dtype, layer0=layer0, q_per_kv=G)
+        K, V = pack(rng.standard_normal((L, B, H, cap, d))), pack(rng.standard_normal((L, B, H, cap, d)))
+        n = cap - 1 if fill is None else fill
+        self.oc.K[...], self.oc.V[...] = unpack(K), unpack(V)
+        self.oc.score[...] = (0.2 + rng.random((L, B, H, cap))).astype(np.float32)
+        self.oc.pos[...] = np.sort(rng.permuted(np.tile(np.arange(2 * cap), (L * B * H, 1)), axis=1)[:, :cap], -1).reshape(L, B, H, cap)
+        self.first = 2 * cap
+        self.oc.len[...] = n
+        # the window's positions are consecutive up to the newest, as a generation leaves them
+        self.oc.pos[..., :n] = np.where(np.arange(n) >= n - n // 3, np.arange(n) - n + self.first, np.minimum(self.oc.pos[..., :n], self.first - n // 3 - 1 - (n - n // 3) + np.arange(n)))
+        for name, t in (("K", K), ("V", V), ("score", self.oc.score), ("pos", self.oc.pos), ("len", self.oc.len)):
+            getattr(self.gc, name).copy_(torch.from_numpy(t))
+        self.ws = kf.new_workspace(self.gc)
+        self.out = torch.zeros((L, B, H * G, d), device="cuda")
+        self.scale = float(1.0 / np.sqrt(np.float32(d)))
+        self.seeds = (np.arange(B) * 7 + seed).astype(np.uint64)
+
+    def token(self, spread=1.0):
+        L, B, H, d = self.oc.L, self.oc.B, self.H, self.oc.d
+        return values(self.rng, (L, B, H * self.G, d), self.dt), values(self.rng, (L, B, H, d), self.dt, spread), values(self.rng, (L, B, H, d), self.dt, spread)
+
+    def oracle(self, q, kn, vn, q_pos, tau, noise, slopes=None, **more):
+        f = [x.float().numpy() for x in (q, kn, vn)]
+        before = self.oc.len.copy()
+        out = self.oc.decode_step(*f, q_pos, tau, self.scale, noise, self.seeds, slopes, q_per_kv=self.G, **more)
+        for u in np.ndindex(*before.shape):  # held in 4 bits from now on
+            self.oc.K[u][before[u]], self.oc.V[u][before[u]] = unpack(pack(f[1][u])), unpack(pack(f[2][u]))
+        return out
+
+    def gpu_args(self, q, kn, vn):
+        return q.cuda(), kn.cuda(), vn.cuda()
+
+    def same(self, what, rtol=2e-5):
+        """State: the same entries (in order, or as a set), rows to the bit, scores within the bound."""
+        lens = host(self.gc.len)
+        np.testing.assert_array_equal(lens, self.oc.len, err_msg=what)
+        pos, score, K, V = host(self.gc.pos).copy(), host(self.gc.score).copy(), self.gc.K.cpu().numpy(), self.gc.V.cpu().numpy()
+        for u in np.ndindex(*lens.shape):
+            m = lens[u]
+            o = np.argsort(pos[u][:m], kind="stable") if self.slot else np.arange(m)
+            np.testing.assert_array_equal(pos[u][:m][o], self.oc.pos[u][:m], err_msg=what)
+            np.testing.assert_array_equal(unpack(K[u][:m][o]), self.oc.K[u][:m], err_msg=what)
+            np.testing.assert_array_equal(unpack(V[u][:m][o]), self.oc.V[u][:m], err_msg=what)
+            score[u][:m] = score[u][:m][o]
+        assert_close_score(score, self.oc.score, lens, what, rtol)
+        # what one step leaves in the last bits does not decide the next: both go on from the same scores
+        for u in np.ndindex(*lens.shape):
+            m = lens[u]
+            o = np.argsort(pos[u][:m], kind="stable") if self.slot else np.arange(m)
+            back = np.empty(m, np.float32)
+            back[o] = self.oc.score[u][:m]
+            self.gc.score[u][:m] = torch.from_numpy(back).cuda()
+
+
+SHAPES = [  # L, B, H, d, cap, G
+    (1, 1, 1, 128, 2, 1), (1, 1, 2, 64, 65, 1), (2, 3, 2, 128, 130, 1), (1, 2, 3, 256, 257, 1), (1, 1, 3, 128, 1023, 1), (1, 2, 8, 64, 999, 1),
+    (1, 1, 2, 128, 700, 2), (2, 1, 3, 256, 321, 2), (1, 2, 2, 64, 129, 4), (1, 1, 2, 128, 513, 4), (1, 1, 2, 256, 200, 4), (1, 2, 1, 64, 300, 8),
+    (2, 1, 2, 128, 260, 8), (1, 1, 2, 256, 301, 8), (4, 8, 40, 64, 70, 1), (1, 1, 1, 128, 9000, 1),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [kf.BF16_Q4, kf.F16_Q4])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_step_and_eviction_match_the_oracle(shape, dtype):
+    L, B, H, d, cap, G = shape
+    k = cap - 1
+    w = k // 3
+    for slot in (False, True):
+        p = Pair(11 + cap + d, L, B, H, d, cap, dtype, G, layer0=3, slot=slot)
+        slopes = (0.5 ** np.arange(1, H * G + 1)).astype(np.float32) * 0.02 if cap % 2 else None
+        for t in range(3):
+            q, kn, vn = p.token(1.0 + t)
+            tau = kf.kf_tau(t, 7)
+            want = p.oracle(q, kn, vn, p.first + t, tau, ko.NOISE_GUMBEL, slopes)
+            kept_ref = p.oc.select_evict(k, w)
+            kept = torch.zeros((L, B, H, k), dtype=torch.int32, device="cuda")
+            kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), p.first + t, cap, tau, p.scale, kf.NOISE_GUMBEL, dev(p.seeds), dev(slopes), p.out,
+                                     k=k, w=w, layout=kf.LAYOUT_SLOT if slot else kf.LAYOUT_ORDERED, kept_idx=kept, workspace=p.ws)
+            assert error_word(p.ws) == 0
+            assert_close_out(host(p.out), want, "step %d" % t)
+            if not slot:
+                np.testing.assert_array_equal(host(kept), kept_ref)
+            p.same("step %d, slot %s" % (t, slot))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("noise", [kf.NOISE_NONE, kf.NOISE_GAUSSIAN, kf.NOISE_CONSTANT])
+def test_step_options(noise):
+    for G, d in ((1, 128), (4, 64)):
+        L, B, H, cap = 2, 3, 2, 80
+        # original and in-cache positions, positions and temperatures of each sequence, a cache that is not full, no m_hint
+        for new_pos in (False, True):
+            p = Pair(5, L, B, H, d, cap, kf.BF16_Q4, G, fill=50)
+            slopes = np.linspace(0.3, 0.01, H * G).astype(np.float32)
+            qp, ts = (p.first + np.arange(B) * 5).astype(np.int32), np.linspace(1.0, 2.0, B).astype(np.float32)
+            q, kn, vn = p.token()
+            want = p.oracle(q, kn, vn, 0, 1.0, noise, slopes, new_pos=new_pos, q_pos_seq=qp, tau_seq=ts)
+            kf.kf_decode_step(p.gc, *p.gpu_args(q, kn, vn), 0, 0, 1.0, p.scale, noise, dev(p.seeds), dev(slopes), p.out, p.ws,
+                              pos_mode=kf.POS_NEW if new_pos else kf.POS_ORIGINAL, seq_q_pos=dev(qp), seq_tau=dev(ts))
+            assert_close_out(host(p.out), want)
+            p.same("options")
+        # one score for all layers
+        p = Pair(6, L, B, H, d, cap, kf.F16_Q4, G)
+        for nm in ("pos", "score"):
+            getattr(p.oc, nm)[1] = getattr(p.oc, nm)[0]
+            getattr(p.gc, nm)[1] = getattr(p.gc, nm)[0]
+        q, kn, vn = p.token()
+        want = p.oracle(q, kn, vn, p.first, 1.25, noise, None, shared=True)
+        p.oc.select_evict(cap - 1, 20)
+        kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), p.first, cap, 1.25, p.scale, noise, dev(p.seeds), None, p.out, k=cap - 1, w=20,
+                                 workspace=p.ws, score_mode=kf.SCORE_SHARED)
+        assert_close_out(host(p.out), want)
+        p.same("shared")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_lengths_of_their_own_full_units_and_far_over_budget(d):
+    cap, k, w = 600, 300, 40
+    lens = np.array([0, 1, 299, 300, 301, 599, 17, 450], np.int32).reshape(1, 2, 4)
+    p = Pair(9, 1, 2, 4, d, cap, kf.BF16_Q4, fill=599)
+    p.oc.len[...] = lens
+    p.gc.len.copy_(torch.from_numpy(lens))
+    for u in np.ndindex(1, 2, 4):
+        p.oc.pos[u] = np.arange(cap)
+    p.gc.pos.copy_(torch.from_numpy(p.oc.pos))
+    q, kn, vn = p.token()
+    want = p.oracle(q, kn, vn, 2 * cap, 1.5, ko.NOISE_GUMBEL)
+    p.oc.select_evict(k, w)
+    kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), 2 * cap, 0, 1.5, p.scale, kf.NOISE_GUMBEL, dev(p.seeds), None, p.out, k=k, w=w, workspace=p.ws)
+    assert error_word(p.ws) == 0
+    assert_close_out(host(p.out), want)
+    p.same("mixed lengths")
+    # a unit without room is left alone, its output cleared, and counted; one that the launch was not shaped for likewise
+    p.gc.len[0, 0, 1], p.gc.len[0, 1, 2] = cap, cap
+    before = [t[0, 0, 1].clone() for t in (p.gc.K, p.gc.V, p.gc.score, p.gc.pos)]
+    p.out.fill_(3.0)
+    kf.kf_decode_step(p.gc, *p.gpu_args(q, kn, vn), 2 * cap + 1, 0, 1.5, p.scale, kf.NOISE_GUMBEL, dev(p.seeds), None, p.out, p.ws)
+    assert error_word(p.ws) == 2 and bool((p.out[0, 0, 1] == 0).all()) and bool((p.out[0, 1, 2] == 0).all())
+    assert all(torch.equal(a, t[0, 0, 1]) for a, t in zip(before, (p.gc.K, p.gc.V, p.gc.score, p.gc.pos)))
+
+
+@pytest.mark.gpu
+def test_eviction_alone_from_far_over_budget_and_fork():
+    for d in (64, 128, 256):
+        L, B, H, cap, k, w = 2, 4, 2, 777, 301, 33
+        p = Pair(13, L, B, H, d, cap, kf.F16_Q4, fill=cap)
+        lens = p.rng.integers(k - 5, cap + 1, (L, B, H)).astype(np.int32)
+        lens[0, 0, 0], lens[1, 1, 1] = cap, k + 1
+        p.oc.len[...] = lens
+        p.gc.len.copy_(torch.from_numpy(lens))
+        ref = p.oc.select_evict(k, w)
+        kept = torch.zeros((L, B, H, k), dtype=torch.int32, device="cuda")
+        kf.kf_select_evict(p.gc, k, w, kept, p.ws)
+        np.testing.assert_array_equal(host(kept), ref)
+        p.same("evict %d" % d)
+        parent = np.array([2, 1, 2, 1], np.int32)
+        p.oc.beam_fork(parent)
+        kf.kf_beam_fork(p.gc, torch.from_numpy(parent).cuda(), p.ws)
+        p.same("fork %d" % d)
+        assert error_word(p.ws) == 0
+
+
+@pytest.mark.gpu
+def test_a_whole_generation_of_beams_over_a_four_bit_cache():
+    """Projection rows -> prompt scores -> eviction into 4 bits -> steps, each followed by the beams' choice and the fork;
+    against the oracle on the values that the rows stand for."""
+    rng = np.random.default_rng(21)
+    R, W, H, d, n, k, w, V, T = 2, 3, 4, 128, 90, 40, 12, 700, 6
+    B = R * W
+    bf = torch.bfloat16
+    freq = (10000.0 ** (-torch.arange(d // 2).float() / (d // 2))).cuda()
+    of = dict(B=B, H=H, d=d, dtype=kf.BF16, rotate=kf.ROTATE_HALVES, rot_dim=d, inv_freq=freq)
+    qkv = values(rng, (B, n, 3 * H, d), bf).cuda()
+    st = qkv.stride()[:2]
+    parts = [qkv[:, :, i * H:(i + 1) * H] for i in range(3)]
+    staged, cache = kf.Cache.allocate(1, B, H, d, n, kf.BF16), kf.Cache.allocate(1, B, H, d, k + 1, kf.BF16_Q4)
+    Q = torch.zeros((1, B, H, n, d), dtype=bf, device="cuda")
+    kf.kf_norm_rotate(kf.Rows(n=n, q_stride=st, k_stride=st, v_stride=st, **of), *parts, Q, staged.K, staged.V)
+    seeds, scale = (np.arange(B) + 3).astype(np.uint64), float(d ** -0.5)
+    ws = kf.new_workspace(staged, n)
+    kf.kf_prefill_score(staged, Q, n, 1.0, scale, kf.NOISE_GUMBEL, dev(seeds), None, ws)
+    kept = torch.zeros((1, B, H, k), dtype=torch.int32, device="cuda")
+    kf.kf_select_evict_into(staged, cache, 0, k, w, kept, ws)
+    oc = ko.OracleCache(1, B, H, d, k + 1, ko.F32)
+    idx = host(kept)
+    for u in np.ndindex(1, B, H):
+        oc.K[u][:k], oc.V[u][:k] = (unpack(pack(t[u].float().cpu().numpy()[idx[u]])) for t in (staged.K, staged.V))
+        oc.pos[u][:k], oc.score[u][:k] = idx[u], host(staged.score)[u][idx[u]]
+    oc.len[...] = k
+    np.testing.assert_array_equal(unpack(cache.K.cpu().numpy())[..., :k, :], oc.K[..., :k, :])
+    ws4 = kf.new_workspace(cache)
+    b = kf.Beams(R=R, W=W, V=V, dtype=kf.BF16, eos=1)
+    wsb = kf.new_beam_workspace(b)
+    score = torch.tensor([0.0, -np.inf, -np.inf] * R, device="cuda")
+    done = torch.zeros(B, dtype=torch.int32, device="cuda")
+    parent, token = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2))
+    out = torch.zeros((1, B, H, d), device="cuda")
+    q1, k1, v1 = (torch.zeros((1, B, H, d), dtype=bf, device="cuda") for _ in range(3))
+    forked = 0
+    for t in range(1, T + 1):
+        x = values(rng, (B, 1, 3 * H, d), bf).cuda()
+        one = kf.Rows(n=1, q_stride=x.stride()[:2], k_stride=x.stride()[:2], v_stride=x.stride()[:2], pos0=n + t - 1, **of)
+        kf.kf_norm_rotate(one, x[:, :, :H], x[:, :, H:2 * H], x[:, :, 2 * H:], q1, k1, v1)
+        kf.kf_decode_select_step(cache, q1, k1, v1, n + t - 1, k + 1, kf.kf_tau(t, T), scale, kf.NOISE_GUMBEL, dev(seeds), None, out, k=k, w=w, workspace=ws4)
+        f = [y.float().cpu().numpy() for y in (q1, k1, v1)]
+        want = oc.decode_step(*f, n + t - 1, kf.kf_tau(t, T), scale, ko.NOISE_GUMBEL, seeds)
+        oc.K[..., k, :], oc.V[..., k, :] = unpack(pack(f[1])), unpack(pack(f[2]))
+        oc.select_evict(k, w)
+        assert_close_out(host(out), want)
+        logits = (out.view(B, H * d) @ torch.randn((H * d, V), generator=torch.Generator(device="cuda").manual_seed(t), device="cuda")).bfloat16()
+        kf.kf_beam_select(b, logits, score, parent, token, score, done=done, new_done=done, workspace=wsb)
+        kf.kf_beam_fork(cache, parent, ws4)
+        oc.beam_fork(host(parent))
+        forked += int((host(parent) != np.arange(B)).sum())
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(host(cache.pos)[..., :k], oc.pos[..., :k], err_msg="step %d" % t)
+        np.testing.assert_array_equal(unpack(cache.K.cpu().numpy())[..., :k, :], oc.K[..., :k, :])
+        # (prompt scores came over as they are; each step adds what the oracle adds)
+        assert_close_score(host(cache.score), oc.score, oc.len, rtol=2e-5 * t)
+    assert error_word(ws4) == 0 and error_word(ws) == 0
+    assert bool((score.view(R, W) > -np.inf).all()) and forked >= 2 * R  # (the first step forks every row but one of a request)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", [kf.LAYOUT_ORDERED, kf.LAYOUT_SLOT])
+@pytest.mark.parametrize("cap", [301, 5001])
+def test_step_number_in_device_memory_replays_and_the_built_in_scratch_agrees(layout, cap):
+    k, n, T = cap - 1, cap + 200, 9
+    p = [Pair(31, 1, 2, 3, 128, cap, kf.BF16_Q4, slot=True) for _ in range(3)]
+    first = p[0].first
+    toks = [p[0].token() for _ in range(4)]
+    now = [x.cuda().clone() for x in toks[0]]
+    step, skipped = torch.ones(1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    seeds = dev(p[0].seeds)
+
+    def call(x):
+        kf.kf_decode_select_step_at(x.gc, *now, first, T, 1.0, 2.0, step, cap, x.scale, kf.NOISE_GUMBEL, seeds, None, x.out, k=k, w=k // 3, layout=layout, workspace=x.ws)
+
+    keep = [t.clone() for t in (p[0].gc.K, p[0].gc.V, p[0].gc.score, p[0].gc.pos, p[0].gc.len)]
+    call(p[0])  # loads the kernels; taken back
+    for t, old in zip((p[0].gc.K, p[0].gc.V, p[0].gc.score, p[0].gc.pos, p[0].gc.len), keep):
+        t.copy_(old)
+    step.fill_(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(p[0])
+    for t, tok in enumerate(toks, 1):
+        for dst, src in zip(now, tok):
+            dst.copy_(src)
+        graph.replay()
+        args = (*now, first + t - 1, cap, kf.kf_tau(t, T), p[1].scale, kf.NOISE_GUMBEL, seeds, None)
+        kf.kf_decode_select_step(p[1].gc, *args, p[1].out, k=k, w=k // 3, layout=layout, workspace=p[1].ws)
+        kf.kf_decode_select_step_noalloc(p[2].gc, *args, p[2].out, k=k, w=k // 3, layout=layout, skipped=skipped)
+        torch.cuda.synchronize()
+        for other in p[1:]:
+            assert torch.equal(p[0].out, other.out), t
+            for name in ("score", "pos", "K", "V"):
+                assert torch.equal(getattr(p[0].gc, name)[:, :, :, :k], getattr(other.gc, name)[:, :, :, :k]), (t, name)
+            assert torch.equal(p[0].gc.len, other.gc.len)
+    assert int(step.item()) == len(toks) + 1 and int(skipped.item()) == 0
+
+
+@pytest.mark.gpu
+def test_separate_calls_equal_the_fused_step_and_leave_what_lies_behind():
+    cap, k, w = 700, 500, 100
+    a, b = (Pair(41, 2, 2, 3, 64, cap, kf.F16_Q4, G=2, fill=k) for _ in range(2))
+    q, kn, vn = a.token()
+    args = (*a.gpu_args(q, kn, vn), a.first, 0, 1.5, a.scale, kf.NOISE_GUMBEL, dev(a.seeds), None)
+    tail = a.gc.K[..., k + 1:, :].clone()
+    kf.kf_decode_select_step(a.gc, *args, a.out, k=k, w=w, workspace=a.ws)
+    kf.kf_decode_step(b.gc, *args, b.out, b.ws)
+    kf.kf_select_evict(b.gc, k, w, None, b.ws)
+    assert torch.equal(a.out, b.out) and torch.equal(a.gc.len, b.gc.len)
+    for name in ("K", "V", "score", "pos"):
+        assert torch.equal(getattr(a.gc, name)[:, :, :, :k], getattr(b.gc, name)[:, :, :, :k]), name
+    assert torch.equal(tail, a.gc.K[..., k + 1:, :])
