@@ -486,8 +486,8 @@ static kf_status prepare_decode(kf_cache* c, const void* q, const void* k_new, c
 // A decode step with its merge.
 static hipError_t decode_whole(const kf_cache* c, const kf::DecodeArgs& a, int64_t U, const kf::DecodePlan& p, hipStream_t stream) {
     if (!kf::is_quant(c->dtype)) return kf::launch_decode(a, U, c->d, c->dtype, p.lds_bytes, stream);
-    const hipError_t e = kf::launch_quant_split(a, U, c->d, c->dtype, stream);
-    return e == hipSuccess ? kf::launch_decode_merge(a, U, c->d, stream) : e;
+    const hipError_t e = kf::launch_quant_step(a, U, c->d, c->dtype, stream);
+    return e == hipSuccess && a.S > 1 ? kf::launch_decode_merge(a, U, c->d, stream) : e;
 }
 
 // Second half of a scoring call with a shared score: the layers' contributions are added up.
@@ -703,16 +703,16 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
     }
     const int64_t U = (int64_t)c->L * c->B * c->H;
     if (layout != KF_LAYOUT_ORDERED || da.shared) few_alone(&da, U);
-    const bool quant = kf::is_quant(c->dtype);  // their split launch always leaves records to merge
+    const bool quant = kf::is_quant(c->dtype);
     if (layout == KF_LAYOUT_ORDERED && !quant && keep_pays(U, k, w, sa.row_bytes)) da.keep_w = w;
     hipError_t e;
     // a few small units: the workgroup that scored one also moves its rows (2 heads x 64 x 64 in fp32, whose two
     // launches were all host and launch time, 17.9 -> 15.7 us a step; 256 units of 64 KB of keys, from a graph, 1.05 to
     // 1.2 times as fast, 16 of 32 KB 1.5); cap: no unit is further over its budget
-    const bool small_ordered = layout == KF_LAYOUT_ORDERED && U <= kWideMaxUnits && c->cap == k + 1 && da.chunk >= k &&
+    const bool small_ordered = !quant && layout == KF_LAYOUT_ORDERED && U <= kWideMaxUnits && c->cap == k + 1 && da.chunk >= k &&
                                (int64_t)k * sa.row_bytes <= kf::kFuseOrderedBytes &&
                                2 * da.G * (int64_t)(da.chunk + 1) * 4 <= 24 * 1024;  // a 4-wave workgroup: see launch_decode_g
-    if (da.S == 1 && !quant && !da.shared && (layout == KF_LAYOUT_SLOT || small_ordered)) {
+    if (da.S == 1 && !da.shared && (layout == KF_LAYOUT_SLOT || small_ordered)) {
         // one workgroup owns each unit and nothing orders the slots, or it orders them: the whole step is one launch
         da.fuse_ordered = layout == KF_LAYOUT_ORDERED;
         if (da.fuse_ordered) da.keep_w = 0;
@@ -720,7 +720,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
         da.fuse_w = w;
         da.fuse_idx = kept_idx;
         if (sched) da.step_inc = step;  // the launch's last workgroup moves the step number on
-        e = kf::launch_decode(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
+        e = decode_whole(c, da, U, p, (hipStream_t)stream);
     } else if (da.shared) {  // shared score: the layers' increments are added up between the merge and the selection
         e = decode_whole(c, da, U, p, (hipStream_t)stream);
         if (e == hipSuccess) e = share_after_decode(c, da, (hipStream_t)stream);
@@ -737,7 +737,7 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
         e = kf::launch_decode_split(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_step_finish(da, sa, U, c->d, (hipStream_t)stream);
         if (e == hipSuccess && sa.rest) e = kf::launch_step_rest(da, sa, U, (hipStream_t)stream);
-    } else if ((da.S > 1 || quant) && (int64_t)da.S * da.chunk <= kTailMergeMaxTokens && !sa.presel) {
+    } else if (da.S > 1 && (int64_t)da.S * da.chunk <= kTailMergeMaxTokens && !sa.presel) {
         // few units in splits: the merge rides in the selection launch, whatever the number of query heads
         if (layout == KF_LAYOUT_SLOT || sa.wide) {
             // the merge has every final score in a register once: it also finds the smallest candidate, and the
@@ -750,12 +750,12 @@ static kf_status fused_step(kf_cache* c, const void* q, const void* k_new, const
             da.pre_slot = sa.ws_pslot;
             sa.presel_done = 1;
         }
-        e = quant ? kf::launch_quant_split(da, U, c->d, c->dtype, (hipStream_t)stream)
+        e = quant ? kf::launch_quant_step(da, U, c->d, c->dtype, (hipStream_t)stream)
                   : kf::launch_decode_split(da, U, c->d, c->dtype, p.lds_bytes, (hipStream_t)stream);
         if (e == hipSuccess) e = kf::launch_step_tail(da, sa, U, c->d, (hipStream_t)stream);
         if (e == hipSuccess && sa.wide) e = kf::launch_shift(sa, U, (hipStream_t)stream);  // few units: rows move in a launch of their own
     } else {  // one workgroup per unit (nothing to merge), or units too long to merge inside the selection
-        if ((da.S > 1 || quant) && sa.presel) {
+        if (da.S > 1 && sa.presel) {
             // few long units: the merge launch, which forms the final scores, also leaves what the selection's
             // candidate scan launch would look for -- one launch less (32 heads x 9.8k tokens: 47.8 -> 41 us per step)
             da.pre_slices = sa.presel = kf::decode_merge_slices(da.S, da.chunk);

@@ -100,10 +100,10 @@ hipError_t launch_decode(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtyp
 // Workgroups per unit of the merge launch that follows a split decode launch.
 int32_t decode_merge_slices(int32_t S, int32_t chunk);
 hipError_t launch_decode_merge(const DecodeArgs& a, int64_t U, int32_t d, hipStream_t stream);  // that launch alone
-// 4-bit caches (kf_quant.hip): the split launch; what follows is the merge of the others.
+// 4-bit caches (kf_quant.hip): one split finishes its unit, several leave records for the merge of the others.
 int32_t quant_max_splits(int64_t U, int32_t m, int32_t d, int32_t G);  // no unit of fewer tokens has more
 DecodePlan plan_quant(int64_t U, int32_t m, int32_t d, int32_t G);
-hipError_t launch_quant_split(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
+hipError_t launch_quant_step(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
 
 // Shared score function: adds up the layers' contributions and gives every layer the same score.
 //   inc != NULL (decode): score[l][bh][j] += sum_l' inc[l'][bh][j] for the m[.][bh] tokens just scored

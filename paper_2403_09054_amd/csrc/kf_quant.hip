@@ -8,22 +8,30 @@
 //
 // The step is that of kf_decode.hip, with the same arguments, workspace records and merge:
 //   x_j = scale*<q, K_j> - slope*(q_pos - pos_j);  out = sum_j softmax(x)_j V_j;  f_j += softmax((x + zeta)/tau)_j
-// A workgroup streams the rows [j0, j1) of one cached head; a lane takes EPL elements of a row (16 bytes of codes, or 8 where
-// many query heads need the registers).  The new token's own key and value enter as they were given, in 16 bits.
+// A workgroup streams the rows [j0, j1) of one cached head: keys through the matrix cores, then values, of which a lane takes EPL
+// elements of a row (16 bytes of codes, or 8 where several query heads need the registers).  The new token's own key and value
+// enter as they were given, in 16 bits.  With a quarter to a third of the bytes of 16-bit rows the launch is close to being bound by
+// its instructions as well as by bytes.  Steps in the slot layout, one launch: 2048 units x 1024 x 128 75 us (4.9 TB/s of rows, scores and
+// positions), 2048 x 2048 x 128 139 us (5.2 TB/s); with 4 query heads 512 x 2048 x 128 71 us (2.6 TB/s).  Non-temporal loads lose 20 %
+// here: a cache line holds pieces of two rows' codes and scales, and is asked for more than once.
 #include "kf_device.h"
 #include "kf_internal.h"
 #include "kf_merge.h"
 
 namespace kf {
 
+
 constexpr int kQuantThreads = 256;
 constexpr int kQuantWaves = kQuantThreads / kWave;
-constexpr int kQuantUnroll = 4;                       // rows a lane has in flight
+constexpr int quant_unroll(int G) { return G == 2 ? 2 : 4; }  // rows a lane has in flight, and as many on their way
 constexpr size_t kQuantLds = 81920 - 1024;            // two workgroups on a compute unit at least
-constexpr int quant_epl(int G) { return G >= 8 ? 16 : 32; }
+constexpr int quant_epl(int G) { return G >= 4 ? 16 : 32; }   // elements of a row that a lane takes
+constexpr int quant_heads(int G) { return G >= 4 ? 4 : G; }   // query heads of a wave
 
 typedef __bf16 q_bf2_t __attribute__((ext_vector_type(2)));
 typedef float q_f2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 q_bf8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------- encoding
 // Scale byte of a group whose largest magnitude is `a`: 255 for one that holds an infinity or a NaN.
@@ -81,15 +89,19 @@ struct QuantPiece {
     static constexpr int W = EPL / 8, SB = EPL / (D / 16);  // words of codes, scale bytes (1, 2, 4 or 8)
     uint32_t w[W];
     uint32_t s[(SB + 3) / 4];
-    __device__ __forceinline__ void load(const char* row, int cl) {
-        if constexpr (W == 4) {
-            const uint4 r = *(const uint4*)(row + cl * 16);
-            w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
+    // codes at voff behind a base that the wave shares, scale bytes at soff
+    __device__ __forceinline__ void load(const char* base, uint32_t voff, uint32_t soff) {
+        if constexpr (W >= 4) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const uint4 r = *(const uint4*)(base + voff + 16 * i);
+                w[4 * i] = r.x, w[4 * i + 1] = r.y, w[4 * i + 2] = r.z, w[4 * i + 3] = r.w;
+            }
         } else {
-            const uint2 r = *(const uint2*)(row + cl * 8);
+            const uint2 r = *(const uint2*)(base + voff);
             w[0] = r.x, w[1] = r.y;
         }
-        const char* sp = row + D / 2 + cl * SB;
+        const char* sp = base + soff;
         if constexpr (SB == 8) {
             const uint2 r = *(const uint2*)sp;
             s[0] = r.x, s[1] = r.y;
@@ -97,9 +109,10 @@ struct QuantPiece {
         else if constexpr (SB == 2) s[0] = *(const uint16_t*)sp;
         else s[0] = *(const uint8_t*)sp;
     }
-    __device__ __forceinline__ float scale(int g) const {  // of the lane's g-th group
+    // of the lane's g-th group; the conversions read the exponent bits of it alone, so that one shift will do
+    __device__ __forceinline__ float scale(int g) const {
         const uint32_t b = s[g / 4];
-        return __uint_as_float(SB == 1 ? b << 23 : ((b >> (8 * (g % 4))) & 255u) << 23);
+        return __uint_as_float(g % 4 == 3 ? b >> 1 : b << (23 - 8 * (g % 4)));
     }
 };
 template <int SEL>
@@ -107,80 +120,55 @@ __device__ __forceinline__ q_bf2_t quant_bf16(uint32_t w, float s) { return __bu
 template <int SEL>
 __device__ __forceinline__ q_f2_t quant_f32(uint32_t w, float s) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, SEL); }
 
-// <q, row piece>: the decoded pairs against a query kept as pairs of bf16; a half of 11 significant bits is the sum of two.
-template <typename T, int EPL>
+// Eight elements of a query as bf16, for the products with decoded pairs; a half's 11 significant bits are the sum of two.
+template <typename T>
 struct QuantQuery {
-    static constexpr int TERMS = sizeof(T) == 2 && ElemTraits<T>::kPerVec == 8 && __is_same(T, f16_t) ? 2 : 1;
-    uint32_t q[TERMS][EPL / 2];
+    static constexpr int TERMS = __is_same(T, f16_t) ? 2 : 1;
+    uint4 q[TERMS];
     __device__ __forceinline__ void load(const T* p) {
+        const uint4 r = *(const uint4*)p;
+        if constexpr (TERMS == 1) {
+            q[0] = r;
+        } else {
+            float f[8];
+            unpack16<T>(r, f);
+            uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int i = 0; i < EPL / 8; ++i) {
-            const uint4 r = ((const uint4*)p)[i];
-            if constexpr (TERMS == 1) {
-                q[0][4 * i] = r.x, q[0][4 * i + 1] = r.y, q[0][4 * i + 2] = r.z, q[0][4 * i + 3] = r.w;
-            } else {
-                float f[8];
-                unpack16<T>(r, f);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t a = __float_as_uint(f[2 * j]), b = __float_as_uint(f[2 * j + 1]);
-                    q[0][4 * i + j] = (a >> 16) | (b & 0xFFFF0000u);  // upper 8 significant bits; the rest is exact too
-                    const float ra = f[2 * j] - __uint_as_float(a & 0xFFFF0000u), rb = f[2 * j + 1] - __uint_as_float(b & 0xFFFF0000u);
-                    q[TERMS - 1][4 * i + j] = (__float_as_uint(ra) >> 16) | (__float_as_uint(rb) & 0xFFFF0000u);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = __float_as_uint(f[2 * j]), b = __float_as_uint(f[2 * j + 1]);
+                hi[j] = (a >> 16) | (b & 0xFFFF0000u);  // upper 8 significant bits; the rest is exact too
+                const float ra = f[2 * j] - __uint_as_float(a & 0xFFFF0000u), rb = f[2 * j + 1] - __uint_as_float(b & 0xFFFF0000u);
+                lo[j] = (__float_as_uint(ra) >> 16) | (__float_as_uint(rb) & 0xFFFF0000u);
             }
+            q[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            q[TERMS - 1] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
-    }
-    __device__ __forceinline__ float dot(const q_bf2_t (&k)[EPL / 2]) const {
-        float p = 0.0f;
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-#pragma unroll
-            for (int i = 0; i < EPL / 2; ++i) p = __builtin_amdgcn_fdot2_f32_bf16(k[i], __builtin_bit_cast(q_bf2_t, q[t][i]), p, false);
-        }
-        return p;
     }
 };
+// The eight elements of word w of a piece, as pairs.
 template <int D, int EPL>
-__device__ __forceinline__ void quant_decode(const QuantPiece<D, EPL>& p, q_bf2_t (&v)[EPL / 2]) {
-#pragma unroll
-    for (int w = 0; w < EPL / 8; ++w) {
-        v[4 * w + 0] = quant_bf16<0>(p.w[w], p.scale((8 * w + 0) / (D / 16)));
-        v[4 * w + 1] = quant_bf16<1>(p.w[w], p.scale((8 * w + 2) / (D / 16)));
-        v[4 * w + 2] = quant_bf16<2>(p.w[w], p.scale((8 * w + 4) / (D / 16)));
-        v[4 * w + 3] = quant_bf16<3>(p.w[w], p.scale((8 * w + 6) / (D / 16)));
-    }
+__device__ __forceinline__ void quant_decode(const QuantPiece<D, EPL>& p, int w, q_bf2_t (&v)[4]) {
+    v[0] = quant_bf16<0>(p.w[w], p.scale((8 * w + 0) / (D / 16)));
+    v[1] = quant_bf16<1>(p.w[w], p.scale((8 * w + 2) / (D / 16)));
+    v[2] = quant_bf16<2>(p.w[w], p.scale((8 * w + 4) / (D / 16)));
+    v[3] = quant_bf16<3>(p.w[w], p.scale((8 * w + 6) / (D / 16)));
 }
 template <int D, int EPL>
-__device__ __forceinline__ void quant_decode(const QuantPiece<D, EPL>& p, q_f2_t (&v)[EPL / 2]) {
-#pragma unroll
-    for (int w = 0; w < EPL / 8; ++w) {
-        v[4 * w + 0] = quant_f32<0>(p.w[w], p.scale((8 * w + 0) / (D / 16)));
-        v[4 * w + 1] = quant_f32<1>(p.w[w], p.scale((8 * w + 2) / (D / 16)));
-        v[4 * w + 2] = quant_f32<2>(p.w[w], p.scale((8 * w + 4) / (D / 16)));
-        v[4 * w + 3] = quant_f32<3>(p.w[w], p.scale((8 * w + 6) / (D / 16)));
-    }
+__device__ __forceinline__ void quant_decode(const QuantPiece<D, EPL>& p, int w, q_f2_t (&v)[4]) {
+    v[0] = quant_f32<0>(p.w[w], p.scale((8 * w + 0) / (D / 16)));
+    v[1] = quant_f32<1>(p.w[w], p.scale((8 * w + 2) / (D / 16)));
+    v[2] = quant_f32<2>(p.w[w], p.scale((8 * w + 4) / (D / 16)));
+    v[3] = quant_f32<3>(p.w[w], p.scale((8 * w + 6) / (D / 16)));
 }
 
 // What a lane O lanes away holds.
 template <int O>
 __device__ __forceinline__ float from_lane_xor(float v) {
-    if constexpr (O == 1) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true));
-    else if constexpr (O == 2) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true));
+    if constexpr (O == 2) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true));
     else if constexpr (O == 4) return __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x101F));
     else if constexpr (O == 8) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xF, 0xF, true));
     else if constexpr (O == 16) return __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F));
     else return __shfl_xor(v, 32, kWave);
-}
-// Sum over the LPR lanes of a row, in every one of them.
-template <int LPR>
-__device__ __forceinline__ float row_sum(float p) {
-    p += from_lane_xor<1>(p);
-    if constexpr (LPR >= 4) p += from_lane_xor<2>(p);
-    if constexpr (LPR >= 8)  // (the lanes of a quad hold the same by now: any lane of the other quad will do)
-        p += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, p), 0x141, 0xF, 0xF, true));
-    if constexpr (LPR >= 16) p += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, p), 0x140, 0xF, 0xF, true));
-    return p;
 }
 // N sums spread over the lanes that differ in bits O, O/2, .. LPR: each step sends half away and adds what comes, so a lane is left
 // with N / (64 / LPR) of them, the ones from `off` on.
@@ -198,18 +186,27 @@ __device__ __forceinline__ void spread_sums(float* v, int lane, int& off) {
     }
 }
 
+// The workgroup: NT / 64 waves over the rows [j0, j1), or, with 8 query heads, four over the rows for heads 0-3 and four for heads
+// 4-7 (a row comes from the cache the second time; 8 heads in one wave would take 128 registers of sums).
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(kQuantThreads) quant_split_kernel(const DecodeArgs a) {
-    constexpr int NT = kQuantThreads, NW = kQuantWaves, UNR = kQuantUnroll, EPL = quant_epl(G), LPR = D / EPL, RPW = kWave / LPR;
-    constexpr int RPB = RPW * NW, TILE = RPB * UNR, PW = D + 4, RB = D / 2 + 16;
+__device__ __forceinline__ void quant_block(const DecodeArgs& a) {
+    constexpr int UNR = quant_unroll(G), EPL = quant_epl(G), HG = quant_heads(G), HS = G / HG, NT = kQuantThreads * HS;
+    constexpr int NW = kQuantWaves, WA = NT / kWave, LPR = D / EPL, RPW = kWave / LPR, RPB = RPW * NW, TILE = RPB * UNR;
+    constexpr int PW = D + 4, RB = D / 2 + 16;
     extern __shared__ float smem[];
-    __shared__ float red[2 * G * NW];
+    __shared__ float red[2 * WA], red_s[2 * WA];
+    __shared__ float stat[4 * G];  // per query head: max x, sum p, max y, sum e
+    __shared__ unsigned long long evict_min[WA];
+    __shared__ int evict_slot;
+    __shared__ float new_score;
     const int CS = a.chunk + 1;
-    float* xs = smem;               // [G][CS] logits, then attention weights
-    float* ys = smem + G * CS;      // [G][CS] adjusted logits / tau, then their exponentials
-    float* red_o = smem + 2 * G * CS;  // [NW][G*D]
+    float* xs = smem;                  // [G][CS] logits, then attention weights
+    float* ys = smem + G * CS;         // [G][CS] adjusted logits / tau, then their exponentials
+    int32_t* ps = (int32_t*)(smem + 2 * G * CS);              // [CS] positions (several query heads)
+    float* red_o = smem + (2 * G + (G > 1 ? 1 : 0)) * CS;     // [NW][G*D]
 
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, sub = lane / LPR, cl = lane % LPR;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), sub = lane / LPR, cl = lane % LPR;
+    const int wr = wv % NW, g0 = wv / NW * HG;  // the wave's share of the rows, its first head
     const int S = a.S;
     const uint32_t ui = blockIdx.x / (uint32_t)S, lb = ui / (uint32_t)a.H;
     const int64_t u = ui;
@@ -221,25 +218,33 @@ __global__ void __launch_bounds__(kQuantThreads) quant_split_kernel(const Decode
     const T* qu = (const T*)a.q + (size_t)u * G * D;
     const T* knew = (const T*)a.k_new + (size_t)u * D;
     const T* vnew = (const T*)a.v_new + (size_t)u * D;
+    float* fu = a.score + (size_t)u * a.cap;
     int32_t* pu = a.pos + (size_t)u * a.cap;
 
-    const uint64_t seed_b = random ? a.seeds[b] : 0;
+    // The words of device memory that the launch depends on, asked for together; an absent one is read from where something else lies.
+    uint64_t seed_b = uniform_load(random ? a.seeds + b : (const uint64_t*)a.q);
+    int32_t step_now = uniform_load(a.step ? a.step : a.len);
+    int32_t seq_pos = uniform_load(a.seq_q_pos ? a.seq_q_pos + b : a.len);
+    float seq_tau = uniform_load(a.seq_tau ? a.seq_tau + b : (const float*)a.len);
+    int len0 = uniform_load(a.len + u);
+    asm volatile("" : "+s"(seed_b), "+s"(step_now), "+s"(seq_pos), "+s"(seq_tau), "+s"(len0));  // (read once)
     int q_pos = a.q_pos;
     float inv_tau = a.inv_tau;
     if (a.step) {  // as in the step over 16-bit caches
-        const int t = max(*a.step, 1);
+        const int t = max(step_now, 1);
         q_pos = a.n0 + t - 1;
         inv_tau = 1.0f / schedule_tau(a.tau_init, a.dtau, min(t, a.T));
     }
-    if (a.seq_q_pos) q_pos = a.seq_q_pos[b];
-    if (a.seq_tau) inv_tau = 1.0f / a.seq_tau[b];
-    const int len0 = a.len[u], m = len0 + 1;
+    if (a.seq_q_pos) q_pos = seq_pos;
+    if (a.seq_tau) inv_tau = 1.0f / seq_tau;
+    const int m = len0 + 1;
     if (len0 < 0 || len0 >= a.cap || len0 > S * a.chunk) {  // no room for the new token: leave the unit alone, report it
         if (s == 0) {
             for (int c = tid; c < G * D; c += NT) a.out[u * G * D + c] = 0.0f;
             if (tid == 0) {
                 atomicAdd(a.ws_err, 1);
                 a.ws_m[u] = 0;
+                if (a.fuse_k > 0 && len0 > a.fuse_k + 1) atomicAdd(a.ws_err, 1);  // the selection would have refused it as well
             }
         }
         return;
@@ -247,54 +252,125 @@ __global__ void __launch_bounds__(kQuantThreads) quant_split_kernel(const Decode
     const int j0 = s * a.chunk, j1 = min(len0, j0 + a.chunk), cnt_c = max(j1 - j0, 0);
     const bool owner = s == S - 1;
     const int cnt = cnt_c + (owner ? 1 : 0);
-
-    // ---- append (nobody reads the row back in this launch)
-    if (owner) {
+    // a step in one launch (one split, slot layout): a unit one token over its budget evicts here, and the new token goes
+    // straight into the freed slot
+    const bool over = a.fuse_k > 0 && m > a.fuse_k, evict_here = over && m == a.fuse_k + 1;
+    auto store_new = [&](int slot) {  // called by all; nobody reads the row back in this launch
         if (tid < 32) {
-            const int g = tid & 15;
-            const size_t at = (size_t)len0 * RB;
-            if (tid < 16) quant_group<T, D>((const char*)knew, Ku + at, g);
-            else quant_group<T, D>((const char*)vnew, Vu + at, g);
+            if (tid < 16) quant_group<T, D>((const char*)knew, Ku + (size_t)slot * RB, tid);
+            else quant_group<T, D>((const char*)vnew, Vu + (size_t)slot * RB, tid - 16);
         }
-        if (tid == 2 * kWave) pu[len0] = q_pos;
-    }
+        if (tid == 2 * kWave) pu[slot] = q_pos;
+    };
+    if (owner && !evict_here) store_new(len0);
 
-    // rows past the split re-read its last one; their logits are dropped, their weights are zero
+    // Rows past the split re-read its last one; their logits are dropped, their weights are zero.  A tile that lies inside is
+    // addressed by one scalar base and offsets that stay the same.
     typedef QuantPiece<D, EPL> Piece;
-    Piece cur[UNR], nxt[UNR];
-    const int base0 = j0 + wv * RPW;
+    Piece ping[UNR], pong[UNR];
+    const int base0 = j0 + wr * RPW;
+    const uint32_t voff = (uint32_t)(sub * RB + cl * (EPL / 2)), soff = (uint32_t)(sub * RB + D / 2 + cl * Piece::SB);
     auto load_tile = [&](const char* rows, int base, Piece(&p)[UNR]) {
+        if (base + (UNR - 1) * RPB + RPW <= j1) {
+            const char* at = rows + (size_t)base * RB;
 #pragma unroll
-        for (int i = 0; i < UNR; ++i) p[i].load(rows + (size_t)min(base + i * RPB + sub, j1 - 1) * RB, cl);
+            for (int i = 0; i < UNR; ++i) p[i].load(at + i * RPB * RB, voff, soff);
+        } else {
+#pragma unroll
+            for (int i = 0; i < UNR; ++i) {
+                const uint32_t at = (uint32_t)((min(base + i * RPB + sub, j1 - 1) - j0) * RB);  // (at least 0: offsets are unsigned)
+                p[i].load(rows + (size_t)j0 * RB, at + cl * (EPL / 2), at + D / 2 + cl * Piece::SB);
+            }
+        }
+    };
+    // The V stream alternates between two sets of registers, one under way while the other is used.
+    auto stream = [&](const char* rows, auto use) {  // the first tile is in `ping`, or on its way there
+        int base = base0;
+        while (base < j1) {
+            if (base + TILE < j1) load_tile(rows, base + TILE, pong);
+            use(base, ping);
+            base += TILE;
+            if (base >= j1) break;
+            if (base + TILE < j1) load_tile(rows, base + TILE, ping);
+            use(base, pong);
+            base += TILE;
+        }
     };
 
     // ---- K: plain products into LDS
     {
-        QuantQuery<T, EPL> q[G];
+        // On the matrix cores, 16 rows by 16 heads (the others zero) a tile.  Lane (i, kb) holds the kb-th quarter of row i, D/4 codes and four scale bytes; the order of a contraction is free, so word w of the
+        // quarters is one 16x16x32 product, with the queries laid out alike.  A lane gets the logits of head i, rows 4*kb .. +3.
+        constexpr int QW = D / 32, TERMS = QuantQuery<T>::TERMS;
+        typedef QuantPiece<D, D / 4> Quarter;
+        const int i16 = lane & 15, kb = lane >> 4;
+        uint4 bq[TERMS][QW];
 #pragma unroll
-        for (int g = 0; g < G; ++g) q[g].load(qu + g * D + cl * EPL);
-        if (base0 < j1) load_tile(Ku, base0, cur);
-        for (int base = base0; base < j1; base += TILE) {
-            if (base + TILE < j1) load_tile(Ku, base + TILE, nxt);
+        for (int w = 0; w < QW; ++w) {
+            QuantQuery<T> one;
+            one.load(qu + min(i16, G - 1) * D + kb * (D / 4) + 8 * w);
 #pragma unroll
-            for (int i = 0; i < UNR; ++i) {
-                q_bf2_t kv[EPL / 2];
-                quant_decode<D, EPL>(cur[i], kv);
-                const int j = base + i * RPB + sub;
+            for (int t = 0; t < TERMS; ++t)
+                bq[t][w] = i16 < G ? one.q[t] : make_uint4(0u, 0u, 0u, 0u);
+        }
+        constexpr int KT = 16 * WA;
+        const char* rows = Ku + (size_t)j0 * RB;
+        auto load = [&](int base, Quarter& q) {
+            const uint32_t at = (uint32_t)((min(base + i16, j1 - 1) - j0) * RB);
+            q.load(rows, at + kb * (D / 8), at + D / 2 + 4 * kb);
+        };
+        auto logits = [&](int base, const Quarter& q) {
+            f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const float p = row_sum<LPR>(q[g].dot(kv));
-                    if (cl == g % LPR && j < j1) xs[g * CS + j - j0] = p;
-                }
+            for (int w = 0; w < QW; ++w) {
+                q_bf2_t kv[4];
+                quant_decode<D, D / 4>(q, w, kv);
+                const q_bf8_t av = __builtin_bit_cast(q_bf8_t, make_uint4(__builtin_bit_cast(uint32_t, kv[0]), __builtin_bit_cast(uint32_t, kv[1]),
+                                                                         __builtin_bit_cast(uint32_t, kv[2]), __builtin_bit_cast(uint32_t, kv[3])));
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(q_bf8_t, bq[t][w]), acc, 0, 0, 0);
             }
+            if (i16 < G) {
+                float* xg = xs + i16 * CS + base - j0 + 4 * kb;
 #pragma unroll
-            for (int i = 0; i < UNR; ++i) cur[i] = nxt[i];
+                for (int r = 0; r < 4; ++r)
+                    if (base + 4 * kb + r < j1) xg[r] = acc[r];
+            }
+        };
+        constexpr int KU = D >= 256 ? 2 : 4;  // tiles a wave has in flight
+        Quarter q[KU];
+        const int kbase = j0 + wv * 16;
+#pragma unroll
+        for (int i = 0; i < KU; ++i)
+            if (kbase + i * KT < j1) load(kbase + i * KT, q[i]);
+        // Several heads: the positions, which the logits' adjustment asks for, on their way behind the first tiles.  (A wave
+        // adjusts a head's tokens, stride after stride, and each waited for a trip to memory: 512 units x 2048 x 128 with 4 query
+        // heads 89.6 us, 79.7 so; one head has four waves, a quarter of the strides, and gains nothing.)
+        if constexpr (G > 1) {
+            for (int t0 = tid; t0 < cnt_c; t0 += 4 * NT) {
+                int32_t pj[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pj[i] = pu[j0 + min(t0 + i * NT, cnt_c - 1)];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t0 + i * NT < cnt_c) ps[t0 + i * NT] = pj[i];
+            }
+            if (tid == 0) ps[cnt_c] = q_pos;
+        }
+        for (int base = kbase; base < j1; base += KU * KT) {
+#pragma unroll
+            for (int i = 0; i < KU; ++i) {
+                if (base + i * KT >= j1) break;
+                logits(base + i * KT, q[i]);
+                if (base + (KU + i) * KT < j1) load(base + (KU + i) * KT, q[i]);
+            }
         }
     }
-    if (owner && wv == NW - 1) {  // the new token's
+    if (owner && wv == WA - 1) {  // the new token's
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float p = 0.0f;
+#pragma unroll
             for (int c = lane; c < D; c += kWave) {
                 float kq[2];
                 if constexpr (__is_same(T, bf16_t)) kq[0] = bf16_lo(knew[c].bits), kq[1] = bf16_lo(qu[g * D + c].bits);
@@ -305,104 +381,101 @@ __global__ void __launch_bounds__(kQuantThreads) quant_split_kernel(const Decode
             if (lane == 0) xs[g * CS + cnt_c] = p;
         }
     }
-    if (base0 < j1) load_tile(Vu, base0, cur);  // in flight while the statistics are formed
+    if (base0 < j1) load_tile(Vu, base0, ping);  // under way while the statistics are formed
     __syncthreads();
 
     // ---- position bias, logit adjustment, the two softmaxes' statistics (base 2)
-    float mx[2 * G], sum[2 * G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const int hq = h * G + g;
+    // A wave takes a head, or a share of one's tokens: WPH waves a head.
+    constexpr int WPH = WA / G;
+    static_assert(WPH >= 1, "a wave for each head");
+    {
+        const int g = wv / WPH, t0 = wv % WPH * kWave + lane, hq = h * G + g;
+        float *xg = xs + g * CS, *yg = ys + g * CS;
         const float slope = a.slopes ? a.slopes[hq] : 0.0f;
         const uint32_t rk = random ? row_key(unit_key(seed_b, (uint32_t)l, (uint32_t)hq), (uint32_t)q_pos) : 0u;
         float m0 = -INFINITY, m1 = -INFINITY;
-        for (int t = tid; t < cnt; t += NT) {
-            const int j = j0 + t, pj = t == cnt_c ? q_pos : pu[j];
-            const int dist = t == cnt_c ? 0 : a.new_pos ? len0 - j : q_pos - pj;
-            const float x = (xs[g * CS + t] * a.scale - slope * (float)dist) * kLog2e;
+        for (int t = t0; t < cnt; t += kWave * WPH) {
+            const int pj = G > 1 ? ps[t] : t == cnt_c ? q_pos : pu[j0 + t];
+            const int dist = t == cnt_c ? 0 : a.new_pos ? len0 - j0 - t : q_pos - pj;
+            const float x = (xg[t] * a.scale - slope * (float)dist) * kLog2e;
             const float y = (x + zeta_log2e(a.noise, rk, (uint32_t)pj)) * inv_tau;
-            xs[g * CS + t] = x;
-            ys[g * CS + t] = y;
+            xg[t] = x;
+            yg[t] = y;
             m0 = fmaxf(m0, x);
             m1 = fmaxf(m1, y);
         }
-        mx[2 * g] = wave_max(m0);
-        mx[2 * g + 1] = wave_max(m1);
-        if (lane == 0) red[2 * G * wv + 2 * g] = mx[2 * g], red[2 * G * wv + 2 * g + 1] = mx[2 * g + 1];
-    }
-    __syncthreads();
+        m0 = wave_max(m0);
+        m1 = wave_max(m1);
+        if constexpr (WPH > 1) {
+            if (lane == 0) red[2 * wv] = m0, red[2 * wv + 1] = m1;
+            __syncthreads();
+            m0 = red[2 * g * WPH], m1 = red[2 * g * WPH + 1];
 #pragma unroll
-    for (int i = 0; i < 2 * G; ++i) {
-        mx[i] = red[i];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) mx[i] = fmaxf(mx[i], red[2 * G * w + i]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
+            for (int w = 1; w < WPH; ++w) m0 = fmaxf(m0, red[2 * (g * WPH + w)]), m1 = fmaxf(m1, red[2 * (g * WPH + w) + 1]);
+        }
         float s0 = 0.0f, s1 = 0.0f;
-        for (int t = tid; t < cnt; t += NT) {
-            const float p = hw_exp2(xs[g * CS + t] - mx[2 * g]), e = hw_exp2(ys[g * CS + t] - mx[2 * g + 1]);
-            xs[g * CS + t] = p;
-            ys[g * CS + t] = e;
+        for (int t = t0; t < cnt; t += kWave * WPH) {
+            const float p = hw_exp2(xg[t] - m0), e = hw_exp2(yg[t] - m1);
+            xg[t] = p;
+            yg[t] = e;
             s0 += p;
             s1 += e;
         }
         s0 = wave_sum(s0);
         s1 = wave_sum(s1);
-        if (lane == 0) red[2 * G * wv + 2 * g] = s0, red[2 * G * wv + 2 * g + 1] = s1;
+        if (lane == 0) {
+            red_s[2 * wv] = s0, red_s[2 * wv + 1] = s1;
+            if (wv % WPH == 0) stat[4 * g] = m0, stat[4 * g + 2] = m1;
+        }
     }
     __syncthreads();  // the weights too
+    if (tid < 2 * G) {  // (read behind the barrier that follows the V stream)
+        float r = red_s[2 * (tid / 2) * WPH + (tid & 1)];
 #pragma unroll
-    for (int i = 0; i < 2 * G; ++i) {
-        sum[i] = red[i];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) sum[i] += red[2 * G * w + i];
+        for (int w = 1; w < WPH; ++w) r += red_s[2 * ((tid / 2) * WPH + w) + (tid & 1)];
+        stat[4 * (tid / 2) + 1 + 2 * (tid & 1)] = r;
     }
 
     // ---- V
-    float acc[G * EPL];
+    float acc[HG * EPL];
 #pragma unroll
-    for (int i = 0; i < G * EPL; ++i) acc[i] = 0.0f;
-    for (int base = base0; base < j1; base += TILE) {
-        if (base + TILE < j1) load_tile(Vu, base + TILE, nxt);
+    for (int i = 0; i < HG * EPL; ++i) acc[i] = 0.0f;
+    stream(Vu, [&](int base, const Piece(&p)[UNR]) {
 #pragma unroll
         for (int i = 0; i < UNR; ++i) {
-            q_f2_t v[EPL / 2];
-            quant_decode<D, EPL>(cur[i], v);
             const int j = base + i * RPB + sub;
+            float weight[HG];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const float p = j < j1 ? xs[g * CS + j - j0] : 0.0f;
+            for (int g = 0; g < HG; ++g) {
+                weight[g] = xs[(g0 + g) * CS + min(j, j1 - 1) - j0];  // (no branch for each)
+                weight[g] = j < j1 ? weight[g] : 0.0f;
+            }
 #pragma unroll
-                for (int e = 0; e < EPL / 2; ++e) {
-                    acc[g * EPL + 2 * e] = fmaf(p, v[e].x, acc[g * EPL + 2 * e]);
-                    acc[g * EPL + 2 * e + 1] = fmaf(p, v[e].y, acc[g * EPL + 2 * e + 1]);
+            for (int w = 0; w < EPL / 8; ++w) {
+                q_f2_t v[4];
+                quant_decode<D, EPL>(p[i], w, v);
+#pragma unroll
+                for (int g = 0; g < HG; ++g) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc[g * EPL + 8 * w + 2 * e] = fmaf(weight[g], v[e].x, acc[g * EPL + 8 * w + 2 * e]);
+                        acc[g * EPL + 8 * w + 2 * e + 1] = fmaf(weight[g], v[e].y, acc[g * EPL + 8 * w + 2 * e + 1]);
+                    }
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-#pragma unroll
-        for (int i = 0; i < UNR; ++i) cur[i] = nxt[i];
-    }
+    });
     int off = 0;
-    spread_sums<G * EPL, 32, LPR>(acc, lane, off);
-    constexpr int LEFT = G * EPL / RPW;
+    spread_sums<HG * EPL, 32, LPR>(acc, lane, off);
+    constexpr int LEFT = HG * EPL / RPW;
 #pragma unroll
     for (int i = 0; i < LEFT; ++i) {
         const int f = off + i;
-        red_o[wv * G * D + (f / EPL) * D + cl * EPL + f % EPL] = acc[i];
+        red_o[wr * G * D + (g0 + f / EPL) * D + cl * EPL + f % EPL] = acc[i];
     }
     __syncthreads();
-
-    // ---- records for the merge
-    float* we = a.ws_e + (size_t)u * G * a.cap;
-    for (int t = tid; t < cnt; t += NT) {
-        const int slot = t == cnt_c ? len0 : j0 + t;
-#pragma unroll
-        for (int g = 0; g < G; ++g) we[(size_t)g * a.cap + slot] = ys[g * CS + t];
-    }
-    float* part = a.ws_part + ((size_t)u * S + s) * G * PW;
-    for (int c = tid; c < G * D; c += NT) {
+    auto output = [&](int c) {  // element c of [G][D], un-normalised
         float o = red_o[c];
 #pragma unroll
         for (int w = 1; w < NW; ++w) o += red_o[w * G * D + c];
@@ -410,12 +483,108 @@ __global__ void __launch_bounds__(kQuantThreads) quant_split_kernel(const Decode
             const uint32_t bits = vnew[c % D].bits;
             o = fmaf(xs[(c / D) * CS + cnt_c], __is_same(T, bf16_t) ? bf16_lo(bits) : f16_lo(bits), o);
         }
-        part[(c / D) * PW + c % D] = o;
-    }
-    if (tid == 0) {
+        return o;
+    };
+    float* we = a.ws_e + (size_t)u * G * a.cap;
+    if (S > 1) {  // ---- records for the merge
+        for (int t = tid; t < cnt; t += NT) {
+            const int slot = t == cnt_c ? len0 : j0 + t;
 #pragma unroll
-        for (int g = 0; g < G; ++g) *(float4*)(part + g * PW + D) = make_float4(mx[2 * g], sum[2 * g], mx[2 * g + 1], sum[2 * g + 1]);
-        if (owner) a.ws_m[u] = m;
+            for (int g = 0; g < G; ++g) we[(size_t)g * a.cap + slot] = ys[g * CS + t];
+        }
+        float* part = a.ws_part + ((size_t)u * S + s) * G * PW;
+        for (int c = tid; c < G * D; c += NT) part[(c / D) * PW + c % D] = output(c);
+        if (tid < 4 * G) part[(tid >> 2) * PW + D + (tid & 3)] = stat[tid];
+        if (tid == 0 && owner) a.ws_m[u] = m;
+        return;
+    }
+    // ---- the whole unit is here: scores, outputs, and the eviction of a step in one launch
+    float inv[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) inv[g] = 1.0f / stat[4 * g + 3];
+    unsigned long long best = ~0ull;  // smallest candidate: lowest score, of equal ones the highest position
+    int best_slot = -1;
+    for (int t = tid; t < cnt; t += NT) {
+        const int slot = t;  // (j0 is 0, the new token's place len0 is cnt_c)
+        float df = 0.0f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) df = fmaf(ys[g * CS + t], inv[g], df);
+        if (evict_here) {
+            float f_new = df;
+            int pj = q_pos;
+            if (t == cnt_c) {
+                new_score = df;
+            } else {
+                f_new = fu[slot] + df;
+                fu[slot] = f_new;
+                pj = pu[slot];
+            }
+            if (pj <= q_pos - a.fuse_w) {
+                const unsigned long long pack = ((unsigned long long)float_key(f_new) << 32) | (uint32_t)(~(uint32_t)pj);
+                if (pack < best) {
+                    best = pack;
+                    best_slot = slot;
+                }
+            }
+        } else if (a.shared) {
+            we[slot] = df;  // summed over the layers by the launch that follows
+        } else if (t == cnt_c) {
+            fu[slot] = df;
+        } else {
+            unsafeAtomicAdd(&fu[slot], df);  // no round trip; one add per address
+        }
+    }
+    for (int c = tid; c < G * D; c += NT) a.out[u * G * D + c] = output(c) / stat[4 * (c / D) + 1];
+    if (!evict_here) {
+        if (tid == 0) {
+            a.len[u] = m;
+            if (a.shared) a.ws_m[u] = m;
+            if (over) atomicAdd(a.ws_err, 1);  // more than one token over budget: appended, not evicted, reported
+        }
+        if (a.fuse_idx && !over) {
+            int32_t* idx = a.fuse_idx + (size_t)u * a.fuse_k;
+            for (int i = tid; i < a.fuse_k; i += NT) idx[i] = i < m ? i : -1;
+        }
+        return;
+    }
+    const unsigned long long mine = best;
+    best = wave_min(best);
+    if (lane == 0) evict_min[wv] = best;
+    if (tid == 0) evict_slot = -1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WA; ++i) best = evict_min[i] < best ? evict_min[i] : best;
+    if (best != ~0ull && mine == best) evict_slot = best_slot;  // positions are unique: one lane
+    __syncthreads();
+    const int e = evict_slot, k = a.fuse_k;
+    if (e < 0) {  // nothing lies outside the window: append after all, leave the unit one over budget and report it
+        store_new(len0);
+        if (tid == 2 * kWave) {
+            fu[len0] = new_score;
+            a.len[u] = m;
+            atomicAdd(a.ws_err, 1);
+        }
+        return;
+    }
+    if (e != len0) {  // e == len0: the new token itself leaves (only without a recent window)
+        store_new(e);
+        if (tid == 2 * kWave) fu[e] = new_score;
+    }
+    if (a.fuse_idx) {
+        int32_t* idx = a.fuse_idx + (size_t)u * k;
+        for (int i = tid; i < k; i += NT) idx[i] = i == e ? k : i;
+    }
+    if (tid == 0) a.len[u] = k;
+}
+
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kQuantThreads* G / quant_heads(G), 4) quant_step_kernel(const DecodeArgs a) {
+    quant_block<T, D, G>(a);
+    if (a.step_inc && threadIdx.x == 0) {  // step number in device memory: the workgroup that is done last moves it on
+        if (atomicAdd(a.ws_ticket, 1) == (int)gridDim.x - 1) {
+            *a.ws_ticket = 0;
+            *a.step_inc += 1;
+        }
     }
 }
 
@@ -464,52 +633,79 @@ hipError_t launch_quant_gather(const GatherArgs& g, int32_t d, int32_t dtype, hi
 
 // ---------------------------------------------------------------- host
 static int quant_rpb(int32_t d, int32_t G) { return kWave / (d / quant_epl(G)) * kQuantWaves; }
-static size_t quant_lds(int32_t G, int64_t chunk, int32_t d) { return (size_t)(2 * G * (chunk + 1) + kQuantWaves * G * d) * sizeof(float); }
+static size_t quant_lds(int32_t G, int64_t chunk, int32_t d) { return (size_t)((2 * G + (G > 1 ? 1 : 0)) * (chunk + 1) + kQuantWaves * G * d) * sizeof(float); }
 
-// Most splits of a unit of up to m tokens (what the records are sized for): enough for 1024 workgroups in all, each of two
-// rounds of rows at least, and as many as the logits in LDS ask for.
+// Most splits of a unit of up to m tokens (what the records are sized for): as many as keep two rounds of rows for each, up
+// to 2048 workgroups in all, and as many as the logits in LDS ask for.
+static void quant_split_range(int64_t U, int64_t rows, int32_t d, int32_t G, int64_t* lo, int64_t* hi) {
+    const int64_t rpb = quant_rpb(d, G);
+    const int64_t fit = (int64_t)((kQuantLds / sizeof(float) - (size_t)kQuantWaves * G * d) / (2 * G + 1) - 1) / rpb * rpb;
+    *lo = (rows + fit - 1) / fit;
+    *hi = (rows + 2 * rpb - 1) / (2 * rpb);
+    const int64_t most = (2048 + U - 1) / U;
+    if (*hi > most) *hi = most;
+    if (*hi > kDecodeMaxSplits) *hi = kDecodeMaxSplits;
+    if (*hi < *lo) *hi = *lo;
+}
 int32_t quant_max_splits(int64_t U, int32_t m, int32_t d, int32_t G) {
-    const int64_t rows = m > 1 ? m - 1 : 1, rpb = quant_rpb(d, G);
-    const int64_t fit = (int64_t)((kQuantLds / sizeof(float) - (size_t)kQuantWaves * G * d) / (2 * G) - 1) / rpb * rpb;
-    const int64_t lo = (rows + fit - 1) / fit, hi = (rows + 2 * rpb - 1) / (2 * rpb);
-    int64_t S = (1024 + U - 1) / U;
-    if (S > hi) S = hi;
-    if (S > kDecodeMaxSplits) S = kDecodeMaxSplits;
-    if (S < lo) S = lo;
-    return (int32_t)S;
+    int64_t lo, hi;
+    quant_split_range(U, m > 1 ? m - 1 : 1, d, G, &lo, &hi);
+    return (int32_t)hi;
 }
 DecodePlan plan_quant(int64_t U, int32_t m, int32_t d, int32_t G) {
     DecodePlan p;
-    const int64_t rows = m > 1 ? m - 1 : 1, rpb = quant_rpb(d, G), S = quant_max_splits(U, m, d, G);
-    p.chunk = (int32_t)(((rows + S - 1) / S + rpb - 1) / rpb * rpb);
-    p.S = (int32_t)((rows + p.chunk - 1) / p.chunk);
+    int64_t lo, hi;
+    const int64_t rows = m > 1 ? m - 1 : 1, rpb = quant_rpb(d, G);
+    quant_split_range(U, rows, d, G, &lo, &hi);
+    // A launch runs in rounds of as many workgroups as fit (registers: 16 waves on a compute unit; LDS); one of r workgroups on a
+    // compute unit takes its chain of trips to memory and a time by its rows that falls short of proportion for small
+    // r; splits add the launch that merges them.  In microseconds, fitted to the shapes below, best split and the next:
+    // 2048 units x 1024 x 128 1 split 75, 2 105, 4 123; 256 x 4096 x 128, 2 heads 4 splits 57, 2 64, 1 91; 512 x 2048 x 128, 4 heads
+    // 4 splits 71, 2 76; 128 x 4000 x 128 8 splits 31, 4 34, 2 41; 16 x 1024 x 256 6 splits 17.4, 16 18, 2 23.
+    const double fixed = 6.0, row = (G == 1 ? 3.4e-5 : G == 2 ? 4e-5 : G == 4 ? 5.6e-5 : 1.1e-4) * (d / 2 + 16);
+    double best = 0.0;
+    for (int64_t S = lo; S <= hi && S <= lo + 63; ++S) {
+        const int64_t chunk = ((rows + S - 1) / S + rpb - 1) / rpb * rpb, n = (rows + chunk - 1) / chunk;
+        const size_t lds = quant_lds(G, chunk, d);
+        if (lds > kQuantLds) continue;
+        int64_t fit = (int64_t)(163840 / (lds + 1024));
+        if (fit > (G == 8 ? 2 : 4)) fit = G == 8 ? 2 : 4;
+        const int64_t each = 256 * fit, full = U * n / each, left = (U * n - full * each + 255) / 256;
+        auto round = [&](int64_t r) { return fixed + row * (double)(chunk * (r + 1)); };
+        const double cost = (double)full * round(fit) + (left ? round(left) : 0.0) + (n > 1 ? 5.0 + 0.01 * (double)U : 0.0);
+        if (best == 0.0 || cost < best) {
+            best = cost;
+            p.S = (int32_t)n;
+            p.chunk = (int32_t)chunk;
+        }
+    }
     p.lds_bytes = quant_lds(G, p.chunk, d);
     return p;
 }
 
 template <typename T, int D>
-static hipError_t launch_quant_split_d(const DecodeArgs& a, int64_t U, hipStream_t st) {
+static hipError_t launch_quant_step_d(const DecodeArgs& a, int64_t U, hipStream_t st) {
     const dim3 grid((unsigned)(U * a.S)), block(kQuantThreads);
     const size_t lds = quant_lds(a.G, a.chunk, D);
     if (lds > kQuantLds || a.S > kDecodeMaxSplits) return hipErrorInvalidValue;
     switch (a.G) {
-        case 1: hipLaunchKernelGGL((quant_split_kernel<T, D, 1>), grid, block, lds, st, a); break;
-        case 2: hipLaunchKernelGGL((quant_split_kernel<T, D, 2>), grid, block, lds, st, a); break;
-        case 4: hipLaunchKernelGGL((quant_split_kernel<T, D, 4>), grid, block, lds, st, a); break;
-        case 8: hipLaunchKernelGGL((quant_split_kernel<T, D, 8>), grid, block, lds, st, a); break;
+        case 1: hipLaunchKernelGGL((quant_step_kernel<T, D, 1>), grid, block, lds, st, a); break;
+        case 2: hipLaunchKernelGGL((quant_step_kernel<T, D, 2>), grid, block, lds, st, a); break;
+        case 4: hipLaunchKernelGGL((quant_step_kernel<T, D, 4>), grid, block, lds, st, a); break;
+        case 8: hipLaunchKernelGGL((quant_step_kernel<T, D, 8>), grid, 2 * kQuantThreads, lds, st, a); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
 }
-hipError_t launch_quant_split(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream) {
+hipError_t launch_quant_step(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream) {
     if (dtype == KF_BF16_Q4) {
-        if (d == 64) return launch_quant_split_d<bf16_t, 64>(a, U, stream);
-        if (d == 128) return launch_quant_split_d<bf16_t, 128>(a, U, stream);
-        if (d == 256) return launch_quant_split_d<bf16_t, 256>(a, U, stream);
+        if (d == 64) return launch_quant_step_d<bf16_t, 64>(a, U, stream);
+        if (d == 128) return launch_quant_step_d<bf16_t, 128>(a, U, stream);
+        if (d == 256) return launch_quant_step_d<bf16_t, 256>(a, U, stream);
     } else if (dtype == KF_F16_Q4) {
-        if (d == 64) return launch_quant_split_d<f16_t, 64>(a, U, stream);
-        if (d == 128) return launch_quant_split_d<f16_t, 128>(a, U, stream);
-        if (d == 256) return launch_quant_split_d<f16_t, 256>(a, U, stream);
+        if (d == 64) return launch_quant_step_d<f16_t, 64>(a, U, stream);
+        if (d == 128) return launch_quant_step_d<f16_t, 128>(a, U, stream);
+        if (d == 256) return launch_quant_step_d<f16_t, 256>(a, U, stream);
     }
     return hipErrorInvalidValue;
 }
