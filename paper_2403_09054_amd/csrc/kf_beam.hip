@@ -6,7 +6,8 @@
 //   slices   a workgroup takes a slice of a row into registers, once, and leaves its largest logit, the sum of its
 //            exponentials and its best W logits in order.  A wave finds the W-th largest of its lanes' maxima by a search
 //            over the bits of the ordered key: at least W logits are as large, and only the lanes above it, fewer than W, hold
-//            larger ones; so a short list holds what can be among the best, whatever the logits are.
+//            larger ones; so a short list holds what can be among the best, whatever the logits are.  The largest of the waves'
+//            keys cuts all four lists.
 //   request  a workgroup takes a request: each row's slices are joined (statistics in 64 bits, lists by taking their
 //            smallest heads), then the rows' lists, totals in 64 bits; then the rows are numbered.
 // What bounds the first launch is the bytes of the logits, the second a chain of short steps: W picks a row, then W picks.
@@ -46,15 +47,16 @@ __device__ __forceinline__ uint4 beam_load16(const T* p) {
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-// Entries of a wave's list: the lanes above the W-th largest maximum hold all of theirs, the equal ones W.
+// Most entries that a wave adds to the list: the lanes above the W-th largest maximum hold all of theirs, the equal ones W.
 constexpr int beam_list_cap(int W, int per_lane) { return (W - 1) * per_lane + W; }
 
 template <typename T, int NL>
 __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs a) {
     constexpr int EPV = ElemTraits<T>::kPerVec, NW = kBeamThreads / kWave, EPL = NL * EPV;
-    extern __shared__ unsigned long long list[];  // [NW][cap]
+    extern __shared__ __attribute__((aligned(16))) unsigned long long list[];  // what can be among the best, and eight more
     __shared__ float w_max[NW];
     __shared__ double w_sum[NW];
+    __shared__ uint32_t w_key[NW];
     __shared__ int w_cnt[NW];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, W = a.W, V = a.V;
     const int64_t row = blockIdx.x / (uint32_t)a.S;
@@ -86,14 +88,22 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
             }
         }
     }
-    auto is_word = [&](int i, int e) { return whole[i] || first[i] + e < V; };
 
     // ---- statistics
-    float lmax = -INFINITY;
+    float vmax[NL], lmax = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
+        vmax[i] = x[i][0];
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) lmax = fmaxf(lmax, x[i][e]);  // (passes over NaN)
+        for (int e = 1; e < EPV; ++e) vmax[i] = fmaxf(vmax[i], x[i][e]);  // (passes over NaN)
+        lmax = fmaxf(lmax, vmax[i]);
+    }
+    // the W-th largest of the lanes' maxima, as a key; 0: fewer lanes hold words
+    const uint32_t lkey = any ? float_key(beam_ordered(lmax)) : 0u;
+    uint32_t T32 = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t t = T32 | (1u << bit);
+        if ((int)__popcll(__ballot(lkey >= t)) >= W) T32 = t;
     }
     const float wmax = wave_max(lmax), ref = wmax == -INFINITY ? 0.0f : wmax;
     double sum = 0.0;
@@ -110,68 +120,80 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
     }
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-
-    // ---- the W-th largest of the lanes' maxima, as a key; 0: fewer lanes hold words
-    const uint32_t lkey = any ? float_key(beam_ordered(lmax)) : 0u;
-    uint32_t T32 = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t t = T32 | (1u << bit);
-        if ((int)__popcll(__ballot(lkey >= t)) >= W) T32 = t;
-    }
-    // ---- what can be among the best W: all above it, and the first W (by word) that equal it
-    const int cap = beam_list_cap(W, EPL);
-    unsigned long long* mine = list + (size_t)wv * cap;
-    int n_gt = 0, n_eq = 0;  // entries so far: larger ones from the front, equal ones from the back
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        uint32_t gt = 0, eq = 0;
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-            const uint32_t key = is_word(i, e) ? float_key(beam_ordered(x[i][e])) : 0u;
-            gt |= (key > T32 ? 1u : 0u) << e;
-            eq |= (key == T32 ? 1u : 0u) << e;
-        }
-        if (T32 == 0) eq = 0;
-        if (__ballot((gt | eq) != 0) == 0) continue;
-        const uint32_t both = (uint32_t)__popc(gt) | ((uint32_t)__popc(eq) << 16), upto = wave_scan(both);
-        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-        int g = n_gt + (int)((upto - both) & 0xFFFFu), q = n_eq + (int)((upto - both) >> 16);
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-            const unsigned long long c = beam_entry(beam_ordered(x[i][e]), first[i] + e);
-            if ((gt >> e) & 1u) mine[min(g++, cap - 1)] = c;
-            if (((eq >> e) & 1u) && q < W) mine[cap - 1 - q++] = c;
-        }
-        n_gt += (int)(all & 0xFFFFu);
-        n_eq = min(W, n_eq + (int)(all >> 16));
-    }
     if (lane == 0) {
         w_max[wv] = wmax;
         w_sum[wv] = sum;
-        w_cnt[wv] = n_gt | (n_eq << 16);
+        w_key[wv] = T32;
     }
     __syncthreads();
-
-    // ---- the slice's best W in order: an entry's place is the number of entries before it
-    unsigned long long* out = a.ws_list + ((size_t)row * a.S + s) * W;
-    int total = 0;
+    // ---- What can be among the slice's best W: the words above the largest of the waves' keys, and, of each wave, the first W (by
+    // word) that equal it.  A wave has fewer than W lanes with words above its own key, so its list is bounded.
 #pragma unroll
-    for (int w = 0; w < NW; ++w) total += (w_cnt[w] & 0xFFFF) + (w_cnt[w] >> 16);
-    auto entry = [&](int w, int j) {
-        const int ng = w_cnt[w] & 0xFFFF;
-        return list[(size_t)w * cap + (j < ng ? j : cap - 1 - (j - ng))];
-    };
-    for (int c = tid; c < total; c += kBeamThreads) {
-        int w = 0, j = c;
-        while (j >= (w_cnt[w] & 0xFFFF) + (w_cnt[w] >> 16)) {
-            j -= (w_cnt[w] & 0xFFFF) + (w_cnt[w] >> 16);
-            ++w;
+    for (int w = 0; w < NW; ++w) T32 = max(T32, w_key[w]);
+    const float cut = __uint_as_float((T32 & 0x80000000u) ? T32 & 0x7FFFFFFFu : ~T32);
+    const bool plain = T32 > 0x007FFFFFu;  // else minus infinity, as which a NaN counts, or less: every word is looked at
+    uint32_t gt[NL], eq[NL];
+    uint32_t n_lane = 0, n_eq = 0;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        gt[i] = eq[i] = 0;
+        if (plain) {
+            if (vmax[i] >= cut) {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) {
+                    gt[i] |= (x[i][e] > cut ? 1u : 0u) << e;
+                    eq[i] |= (x[i][e] == cut ? 1u : 0u) << e;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+                if (!whole[i] && first[i] + e >= V) continue;
+                const uint32_t key = float_key(beam_ordered(x[i][e]));
+                gt[i] |= (key > T32 ? 1u : 0u) << e;
+                eq[i] |= (key == T32 ? 1u : 0u) << e;
+            }
         }
-        const unsigned long long v = entry(w, j);
+        // equal ones in the order of words, vector by vector: the bits of the first W stay
+        if (__ballot(eq[i] != 0) != 0) {
+            const uint32_t c = (uint32_t)__popc(eq[i]), upto = wave_scan(c);
+            uint32_t before = n_eq + upto - c;
+            n_eq += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+            for (uint32_t left = eq[i]; left != 0; left &= left - 1, ++before)
+                if (before >= (uint32_t)W) eq[i] &= ~(left & (0u - left));
+        }
+        gt[i] |= eq[i];
+        n_lane += (uint32_t)__popc(gt[i]);
+    }
+    const uint32_t upto = wave_scan(n_lane);
+    if (lane == 63) w_cnt[wv] = (int)upto;
+    __syncthreads();
+    int at = (int)(upto - n_lane), total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        at += w < wv ? w_cnt[w] : 0;
+        total += w_cnt[w];
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        if (gt[i] == 0) continue;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+            if ((gt[i] >> e) & 1u) list[at++] = beam_entry(beam_ordered(x[i][e]), first[i] + e);
+    }
+    if (tid < 8) list[total + tid] = kBeamNone;
+    __syncthreads();
+    // ---- in order: an entry's place is the number of entries before it, eight a step
+    unsigned long long* out = a.ws_list + ((size_t)row * a.S + s) * W;
+    for (int c = tid; c < total; c += kBeamThreads) {
+        const unsigned long long v = list[c];
         int place = 0;
-        for (int w2 = 0; w2 < NW; ++w2) {
-            const int cnt = (w_cnt[w2] & 0xFFFF) + (w_cnt[w2] >> 16);
-            for (int i = 0; i < cnt; ++i) place += entry(w2, i) < v ? 1 : 0;
+        for (int i = 0; i < total; i += 8) {
+            ulonglong2 r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = *(const ulonglong2*)&list[i + 2 * j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) place += (r[j].x < v ? 1 : 0) + (r[j].y < v ? 1 : 0);
         }
         if (place < W) out[place] = v;
     }
@@ -308,7 +330,7 @@ BeamPlan plan_beam(int64_t rows, int32_t W, int32_t V, int32_t dtype) {
         if (S <= kWave && rows * S <= 2048) break;
     }
     p.S = (int32_t)((vecs + p.NL * kBeamThreads - 1) / (p.NL * kBeamThreads));
-    p.lds_slice = (size_t)(kBeamThreads / kWave) * beam_list_cap(W, p.NL * epv) * 8;
+    p.lds_slice = ((size_t)(kBeamThreads / kWave) * beam_list_cap(W, p.NL * epv) + 8) * 8;
     const size_t per_row = (size_t)p.S * W * 8;
     p.waves = W < 16 ? W : 16;
     while (p.waves > 1 && p.waves * per_row > kBeamListLds) --p.waves;
