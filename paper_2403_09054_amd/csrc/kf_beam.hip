@@ -17,7 +17,7 @@
 namespace kf {
 
 constexpr int kBeamThreads = 256;
-constexpr unsigned long long kBeamNone = ~0ull;  // behind every entry: (inverted key of the logit, word), the best is the smallest
+constexpr unsigned long long kBeamNone = ~0ull;  // behind every entry and total: (inverted key of the logit, word), the best is the smallest
 
 __device__ __forceinline__ unsigned long long beam_entry(float x, int v) {
     return ((unsigned long long)(~float_key(x)) << 32) | (uint32_t)v;
@@ -52,7 +52,7 @@ constexpr int beam_list_cap(int W, int per_lane) { return (W - 1) * per_lane + W
 
 template <typename T, int NL>
 __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs a) {
-    constexpr int EPV = ElemTraits<T>::kPerVec, NW = kBeamThreads / kWave, EPL = NL * EPV;
+    constexpr int EPV = ElemTraits<T>::kPerVec, NW = kBeamThreads / kWave;
     extern __shared__ __attribute__((aligned(16))) unsigned long long list[];  // what can be among the best, and eight more
     __shared__ float w_max[NW];
     __shared__ double w_sum[NW];
@@ -221,17 +221,50 @@ __device__ __forceinline__ double key_total(unsigned long long k) {
     return __longlong_as_double((long long)((o >> 63) ? (o & 0x7FFFFFFFFFFFFFFFull) : ~o));
 }
 
+// Smallest of the lanes' values, 32 bits.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t min32_step(uint32_t v) { return min(v, dpp_or<CTRL, ROWS>(~0u, v)); }
+__device__ __forceinline__ uint32_t wave_min32(uint32_t v) {
+    v = min32_step<0x111, 0xF>(v);
+    v = min32_step<0x112, 0xF>(v);
+    v = min32_step<0x114, 0xF>(v);
+    v = min32_step<0x118, 0xF>(v);
+    v = min32_step<0x142, 0xA>(v);
+    v = min32_step<0x143, 0xC>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// ... of 64-bit values, by halves: a chain of 32-bit minima is a third of one of 64-bit ones.
+__device__ __forceinline__ unsigned long long wave_min_halves(unsigned long long v) {
+    const uint32_t hi = wave_min32((uint32_t)(v >> 32));
+    const uint32_t lo = wave_min32((uint32_t)(v >> 32) == hi ? (uint32_t)v : ~0u);
+    return ((unsigned long long)hi << 32) | lo;
+}
+__device__ __forceinline__ void wave_sync_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __global__ void __launch_bounds__(1024) beam_request_kernel(const BeamArgs a) {
     extern __shared__ unsigned long long lists[];  // [waves][S][W]
-    __shared__ unsigned long long best[kBeamMaxW][kBeamMaxW];  // a row's best W
-    __shared__ double lse[kBeamMaxW];
+    __shared__ unsigned long long best[kBeamMaxW][kBeamMaxW];      // a row's best W
+    __shared__ unsigned long long totals[kBeamMaxW][kBeamMaxW];    // ... and their totals' keys
     __shared__ int p_s[kBeamMaxW], tok_s[kBeamMaxW];
     __shared__ double tot_s[kBeamMaxW];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, waves = blockDim.x >> 6, W = a.W, S = a.S;
     const int64_t row0 = (int64_t)blockIdx.x * W;
     for (int i = wv; i < W; i += waves) {
         const int64_t row = row0 + i;
-        if (a.done && a.done[row]) continue;
+        const double sc = (double)a.score[row];
+        if (a.done && a.done[row]) {  // one continuation, at its own score
+            if (lane < W) {
+                best[i][lane] = (unsigned long long)(uint32_t)a.eos;
+                totals[i][lane] = lane == 0 ? total_key(sc) : kBeamNone;
+            }
+            continue;
+        }
+        unsigned long long* mine = lists + (size_t)wv * S * W;
+        for (int j = lane; j < S * W; j += kWave) mine[j] = a.ws_list[(size_t)row * S * W + j];
         // statistics: a lane a slice (S <= 64)
         double m = -INFINITY, sum = 0.0;
         if (lane < S) {
@@ -243,51 +276,47 @@ __global__ void __launch_bounds__(1024) beam_request_kernel(const BeamArgs a) {
         sum = (m == -INFINITY && M != -INFINITY) ? sum * 0.0 : sum * exp(m == M ? 0.0 : m - M);
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-        if (lane == 0) lse[i] = M + log(sum);
+        const double lse = M + log(sum);
         // the slices' lists: a lane a list, the smallest head leaves
-        unsigned long long* mine = lists + (size_t)wv * S * W;
-        for (int j = lane; j < S * W; j += kWave) mine[j] = a.ws_list[(size_t)row * S * W + j];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_sync_lds();
         int at = 0;
         unsigned long long head = lane < S ? mine[lane * W] : kBeamNone;
         for (int j = 0; j < W; ++j) {
-            const unsigned long long c = wave_min(head);
+            const unsigned long long c = wave_min_halves(head);
             if (lane == 0) best[i][j] = c;
             if (c != kBeamNone && head == c) {  // (words are unique: one lane)
                 ++at;
                 head = at < W ? mine[lane * W + at] : kBeamNone;
             }
         }
+        wave_sync_lds();
+        if (lane < W) {
+            const unsigned long long c = best[i][lane];
+            totals[i][lane] = c == kBeamNone ? kBeamNone : total_key(sc + ((double)beam_logit(c) - lse));
+        }
     }
     __syncthreads();
     if (wv != 0) return;
     // ---- the request's best W: a lane a beam
-    const int64_t row = row0 + lane;
-    const bool ended = lane < W && a.done && a.done[row];
-    const double sc = lane < W ? (double)a.score[row] : 0.0;
-    auto head_of = [&](int j) -> unsigned long long {
-        if (lane >= W || j >= W) return kBeamNone;
-        if (ended) return j == 0 ? total_key(sc) : kBeamNone;
-        const unsigned long long c = best[lane][j];
-        return c == kBeamNone ? kBeamNone : total_key(sc + ((double)beam_logit(c) - lse[lane]));
-    };
     int at = 0;
-    unsigned long long head = head_of(0);
+    unsigned long long head = lane < W ? totals[lane][0] : kBeamNone;
     for (int j = 0; j < W; ++j) {
-        const unsigned long long c = wave_min(head);
+        const unsigned long long c = wave_min_halves(head);
         const int owner = __ffsll((long long)__ballot(head == c)) - 1;  // the lowest beam of equals
         if (lane == owner) {
-            p_s[j] = lane;
-            tok_s[j] = ended ? a.eos : (int)(uint32_t)(best[lane][at] & 0xFFFFFFFFull);
+            p_s[j] = lane | (at << 8);
             tot_s[j] = key_total(c);
-            head = head_of(++at);
+            ++at;
+            head = lane < W && at < W ? totals[lane][at] : kBeamNone;
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_sync_lds();
+    if (lane < W) {
+        const int p = p_s[lane];
+        tok_s[lane] = (int)(uint32_t)(best[p & 255][p >> 8] & 0xFFFFFFFFull);
+        p_s[lane] = p & 255;
+    }
+    wave_sync_lds();
     // ---- numbering: a beam's best continuation keeps its row, the others take the rows that died, in order
     const int p = lane < W ? p_s[lane] : -1;
     bool first = lane < W, used = false;
@@ -312,9 +341,7 @@ __global__ void __launch_bounds__(1024) beam_request_kernel(const BeamArgs a) {
         if (a.new_done) p_s[lane] = was || tok_s[lane] == a.eos, tok_s[lane] = r;  // stored below: `done` may be the same array
     }
     if (a.new_done) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_sync_lds();
         if (lane < W) a.new_done[row0 + tok_s[lane]] = p_s[lane];
     }
 }
