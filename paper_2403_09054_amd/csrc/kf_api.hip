@@ -424,6 +424,8 @@ static kf_status prepare_decode(kf_cache* c, const void* q, const void* k_new, c
     if (!a->few) p = plan_step(U, c, m_hint);
     // the partial-record region is sized for the plan at m = cap, the largest
     const int32_t most = max_splits(U, c);
+    if (kf::is_quant(c->dtype) && p.S > kf::kMaxSplits)
+        return fail(KF_EUNSUPPORTED, "units of %d tokens take %d splits, at most %d are built", m_hint, p.S, kf::kMaxSplits);
     if (!a->few && p.S > most) return fail(KF_EWORKSPACE, "internal: split count %d exceeds the sized %d", p.S, most);
     if (U * p.S > kMaxGrid)
         return fail(KF_EUNSUPPORTED, "%lld units in %d splits each exceed the largest launch", (long long)U, p.S);

@@ -10,7 +10,9 @@
 //            keys cuts all four lists.
 //   request  a workgroup takes a request: each row's slices are joined (statistics in 64 bits, lists by taking their
 //            smallest heads), then the rows' lists, totals in 64 bits; then the rows are numbered.
-// What bounds the first launch is the bytes of the logits, the second a chain of short steps: W picks a row, then W picks.
+// What bounds the first launch is its instructions, about 1000 a wave for 2048 words (64 x 4 rows x 50304 in fp32 18 us, 2.8 TB/s;
+// 16 x 16 x 128000 in halves, a fifth of the rows ended, 32 us), the second a chain of short steps, W picks a row, then W
+// picks (4 beams 5.5 us, 16 beams 13.6).
 #include "kf_device.h"
 #include "kf_internal.h"
 
@@ -57,7 +59,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
     __shared__ float w_max[NW];
     __shared__ double w_sum[NW];
     __shared__ uint32_t w_key[NW];
-    __shared__ int w_cnt[NW];
+    __shared__ int w_cnt[NW], s_cnt;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, W = a.W, V = a.V;
     const int64_t row = blockIdx.x / (uint32_t)a.S;
     const int s = (int)(blockIdx.x % (uint32_t)a.S);
@@ -125,6 +127,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
         w_sum[wv] = sum;
         w_key[wv] = T32;
     }
+    if (tid == 0) s_cnt = 0;
     __syncthreads();
     // ---- What can be among the slice's best W: the words above the largest of the waves' keys, and, of each wave, the first W (by
     // word) that equal it.  A wave has fewer than W lanes with words above its own key, so its list is bounded.
@@ -132,20 +135,32 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
     for (int w = 0; w < NW; ++w) T32 = max(T32, w_key[w]);
     const float cut = __uint_as_float((T32 & 0x80000000u) ? T32 & 0x7FFFFFFFu : ~T32);
     const bool plain = T32 > 0x007FFFFFu;  // else minus infinity, as which a NaN counts, or less: every word is looked at
-    uint32_t gt[NL], eq[NL];
-    uint32_t n_lane = 0, n_eq = 0;
+    // Usually those are few: every word that reaches the key, in any order (a branch that most of a wave's words skip; bits of each
+    // word, and a list from them, took half of the kernel's instructions).  Many that equal it, or minus infinity as the
+    // key: the lists with their bounds.
+    const int room = NW * beam_list_cap(W, NL * EPV);
+    int total = room + 1;
+    if (plain) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        gt[i] = eq[i] = 0;
-        if (plain) {
-            if (vmax[i] >= cut) {
+        for (int i = 0; i < NL; ++i) {
+            if (vmax[i] < cut) continue;
 #pragma unroll
-                for (int e = 0; e < EPV; ++e) {
-                    gt[i] |= (x[i][e] > cut ? 1u : 0u) << e;
-                    eq[i] |= (x[i][e] == cut ? 1u : 0u) << e;
+            for (int e = 0; e < EPV; ++e) {
+                if (x[i][e] >= cut) {
+                    const int at = atomicAdd(&s_cnt, 1);
+                    if (at < room) list[at] = beam_entry(beam_ordered(x[i][e]), first[i] + e);
                 }
             }
-        } else {
+        }
+        __syncthreads();
+        total = s_cnt;
+    }
+    if (total > room) {
+        uint32_t gt[NL], eq[NL];
+        uint32_t n_lane = 0, n_eq = 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            gt[i] = eq[i] = 0;
 #pragma unroll
             for (int e = 0; e < EPV; ++e) {
                 if (!whole[i] && first[i] + e >= V) continue;
@@ -153,33 +168,34 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs
                 gt[i] |= (key > T32 ? 1u : 0u) << e;
                 eq[i] |= (key == T32 ? 1u : 0u) << e;
             }
+            // equal ones in the order of words, vector by vector: the bits of the first W stay
+            if (__ballot(eq[i] != 0) != 0) {
+                const uint32_t c = (uint32_t)__popc(eq[i]), upto = wave_scan(c);
+                uint32_t before = n_eq + upto - c;
+                n_eq += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+                for (uint32_t left = eq[i]; left != 0; left &= left - 1, ++before)
+                    if (before >= (uint32_t)W) eq[i] &= ~(left & (0u - left));
+            }
+            gt[i] |= eq[i];
+            n_lane += (uint32_t)__popc(gt[i]);
         }
-        // equal ones in the order of words, vector by vector: the bits of the first W stay
-        if (__ballot(eq[i] != 0) != 0) {
-            const uint32_t c = (uint32_t)__popc(eq[i]), upto = wave_scan(c);
-            uint32_t before = n_eq + upto - c;
-            n_eq += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-            for (uint32_t left = eq[i]; left != 0; left &= left - 1, ++before)
-                if (before >= (uint32_t)W) eq[i] &= ~(left & (0u - left));
+        const uint32_t upto = wave_scan(n_lane);
+        if (lane == 63) w_cnt[wv] = (int)upto;
+        __syncthreads();
+        int at = (int)(upto - n_lane);
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            at += w < wv ? w_cnt[w] : 0;
+            total += w_cnt[w];
         }
-        gt[i] |= eq[i];
-        n_lane += (uint32_t)__popc(gt[i]);
-    }
-    const uint32_t upto = wave_scan(n_lane);
-    if (lane == 63) w_cnt[wv] = (int)upto;
-    __syncthreads();
-    int at = (int)(upto - n_lane), total = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        at += w < wv ? w_cnt[w] : 0;
-        total += w_cnt[w];
-    }
+        for (int i = 0; i < NL; ++i) {
+            if (gt[i] == 0) continue;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        if (gt[i] == 0) continue;
-#pragma unroll
-        for (int e = 0; e < EPV; ++e)
-            if ((gt[i] >> e) & 1u) list[at++] = beam_entry(beam_ordered(x[i][e]), first[i] + e);
+            for (int e = 0; e < EPV; ++e)
+                if ((gt[i] >> e) & 1u) list[at++] = beam_entry(beam_ordered(x[i][e]), first[i] + e);
+        }
     }
     if (tid < 8) list[total + tid] = kBeamNone;
     __syncthreads();

@@ -101,6 +101,7 @@ hipError_t launch_decode(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtyp
 int32_t decode_merge_slices(int32_t S, int32_t chunk);
 hipError_t launch_decode_merge(const DecodeArgs& a, int64_t U, int32_t d, hipStream_t stream);  // that launch alone
 // 4-bit caches (kf_quant.hip): one split finishes its unit, several leave records for the merge of the others.
+constexpr int32_t kMaxSplits = 256;  // of a unit: what the merge holds
 int32_t quant_max_splits(int64_t U, int32_t m, int32_t d, int32_t G);  // no unit of fewer tokens has more
 DecodePlan plan_quant(int64_t U, int32_t m, int32_t d, int32_t G);
 hipError_t launch_quant_step(const DecodeArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);

@@ -6,7 +6,7 @@
 
 namespace kf {
 
-constexpr int kDecodeMaxSplits = 256;  // a wave merges one head's records: this many / 64 per lane, in registers
+constexpr int kDecodeMaxSplits = kMaxSplits;  // a wave merges one head's records: this many / 64 per lane, in registers
 
 // Merges the S partial records of unit u (one per split and query head):
 // rescales every split's un-normalised output and score increments to the

@@ -303,18 +303,20 @@ def test_step_options(noise):
                               pos_mode=kf.POS_NEW if new_pos else kf.POS_ORIGINAL, seq_q_pos=dev(qp), seq_tau=dev(ts))
             assert_close_out(host(p.out), want)
             p.same("options")
-        # one score for all layers
-        p = Pair(6, L, B, H, d, cap, kf.F16_Q4, G)
-        for nm in ("pos", "score"):
-            getattr(p.oc, nm)[1] = getattr(p.oc, nm)[0]
-            getattr(p.gc, nm)[1] = getattr(p.gc, nm)[0]
-        q, kn, vn = p.token()
-        want = p.oracle(q, kn, vn, p.first, 1.25, noise, None, shared=True)
-        p.oc.select_evict(cap - 1, 20)
-        kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), p.first, cap, 1.25, p.scale, noise, dev(p.seeds), None, p.out, k=cap - 1, w=20,
-                                 workspace=p.ws, score_mode=kf.SCORE_SHARED)
-        assert_close_out(host(p.out), want)
-        p.same("shared")
+        # one score for all layers, by one workgroup a unit and in splits
+        for cap in (80, 3000):
+            p = Pair(6, L, B, H, d, cap, kf.F16_Q4, G)
+            assert (kf.kf_decode_launch_shape(p.gc, cap)[0] > 1) == (cap == 3000)
+            for nm in ("pos", "score"):
+                getattr(p.oc, nm)[1] = getattr(p.oc, nm)[0]
+                getattr(p.gc, nm)[1] = getattr(p.gc, nm)[0]
+            q, kn, vn = p.token()
+            want = p.oracle(q, kn, vn, p.first, 1.25, noise, None, shared=True)
+            p.oc.select_evict(cap - 1, 20)
+            kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), p.first, cap, 1.25, p.scale, noise, dev(p.seeds), None, p.out, k=cap - 1, w=20,
+                                     workspace=p.ws, score_mode=kf.SCORE_SHARED)
+            assert_close_out(host(p.out), want)
+            p.same("shared")
 
 
 @pytest.mark.gpu
@@ -480,3 +482,55 @@ def test_separate_calls_equal_the_fused_step_and_leave_what_lies_behind():
     for name in ("K", "V", "score", "pos"):
         assert torch.equal(getattr(a.gc, name)[:, :, :, :k], getattr(b.gc, name)[:, :, :, :k]), name
     assert torch.equal(tail, a.gc.K[..., k + 1:, :])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G,d", [(1, 128), (2, 64), (4, 256), (8, 128)])
+def test_one_launch_steps_treat_units_of_all_lengths_as_the_separate_calls_do(G, d):
+    """Slot layout, one workgroup a unit: empty units, within budget, at it, over it by one and by more, full; no window."""
+    cap, k = 70, 60
+    lens = torch.tensor([0, 1, 30, 59, 60, 61, 69, 70], dtype=torch.int32)
+    for w in (0, 7, 60):
+        a, b = (Pair(51, 1, 8, 9, d, cap, kf.BF16_Q4, G, fill=cap) for _ in range(2))
+        q, kn, vn = a.token()
+        kept = [torch.zeros((1, 8, 9, k), dtype=torch.int32, device="cuda") for _ in range(2)]
+        for p in (a, b):
+            p.gc.len.copy_(lens.view(1, 8, 1).expand(1, 8, 9))
+            p.gc.pos.copy_(torch.arange(cap, dtype=torch.int32).expand(1, 8, 9, cap))
+        q_pos = torch.clamp(lens, max=cap).numpy().astype(np.int32)  # the position behind each sequence's last
+        args = (*a.gpu_args(q, kn, vn), 0, 0, 1.5, a.scale, kf.NOISE_GUMBEL, dev(a.seeds), None)
+        assert kf.kf_decode_launch_shape(a.gc, 0)[0] == 1
+        kf.kf_decode_select_step(a.gc, *args, a.out, k=k, w=w, layout=kf.LAYOUT_SLOT, kept_idx=kept[0], workspace=a.ws, seq_q_pos=dev(q_pos))
+        kf.kf_decode_step(b.gc, *args, b.out, b.ws, seq_q_pos=dev(q_pos))
+        kf.kf_select_evict(b.gc, k, w, kept[1], b.ws, layout=kf.LAYOUT_SLOT)
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, b.out) and torch.equal(a.gc.len, b.gc.len) and error_word(a.ws) == error_word(b.ws)
+        after = a.gc.len.cpu().numpy()
+        for u in np.ndindex(1, 8, 9):
+            m = min(int(after[u]), cap)
+            for name in ("K", "V", "pos"):
+                assert torch.equal(getattr(a.gc, name)[u][:m], getattr(b.gc, name)[u][:m]), (w, u, name)
+            # (the separate calls add to the scores by atomic additions, this one reads and adds: the same sums)
+            assert torch.equal(a.gc.score[u][:m], b.gc.score[u][:m]), (w, u)
+            if m <= k:
+                assert torch.equal(kept[0][u], kept[1][u]), (w, u)
+
+
+@pytest.mark.gpu
+def test_eviction_from_one_four_bit_cache_into_another():
+    for d in (64, 128, 256):
+        p = Pair(61, 2, 1, 3, d, 333, kf.BF16_Q4, fill=333)
+        dst = kf.Cache.allocate(2, 1, 3, d, 101, kf.BF16_Q4)
+        kept = torch.zeros((2, 1, 3, 100), dtype=torch.int32, device="cuda")
+        kf.kf_select_evict_into(p.gc, dst, 0, 100, 30, kept, p.ws)
+        ref = p.oc.select_evict(100, 30)
+        np.testing.assert_array_equal(host(kept), ref)
+        np.testing.assert_array_equal(unpack(dst.K.cpu().numpy())[..., :100, :], p.oc.K[..., :100, :])
+        np.testing.assert_array_equal(unpack(dst.V.cpu().numpy())[..., :100, :], p.oc.V[..., :100, :])
+        np.testing.assert_array_equal(host(dst.score)[..., :100], p.oc.score[..., :100])
+        np.testing.assert_array_equal(host(dst.pos)[..., :100], p.oc.pos[..., :100])
+
+
+def test_units_too_long_for_the_splits_are_refused():
+    c = kf.Cache(K=0x10000, V=0x20000, score=0x30000, pos=0x40000, len=0x50000, L=1, B=1, H=1, d=256, cap=300000, dtype=kf.BF16_Q4, q_per_kv=8)
+    expect(binding.KF_EUNSUPPORTED, kf.kf_decode_step, c, 0x1000, 0x2000, 0x3000, 10, 0, 1.5, 0.1, seeds=0x4000, out=0x5000, workspace=(0x100000, 1 << 40), stream=0)
