@@ -10,8 +10,8 @@
 //            keys cuts all four lists.
 //   request  a workgroup takes a request: each row's slices are joined (statistics in 64 bits, lists by taking their
 //            smallest heads), then the rows' lists, totals in 64 bits; then the rows are numbered.
-// What bounds the first launch is its instructions, about 1000 a wave for 2048 words (64 x 4 rows x 50304 in fp32 18 us, 2.8 TB/s;
-// 16 x 16 x 128000 in halves, a fifth of the rows ended, 32 us), the second a chain of short steps, W picks a row, then W
+// What bounds the first launch is its instructions, 700 to 900 a wave for 2048 words (64 x 4 rows x 50304 in fp32 16 us, 3.2 TB/s;
+// 16 x 16 x 128000 in halves, a fifth of the rows ended, 28 us), the second a chain of short steps, W picks a row, then W
 // picks (4 beams 5.5 us, 16 beams 13.6).
 #include "kf_device.h"
 #include "kf_internal.h"
@@ -52,8 +52,9 @@ __device__ __forceinline__ uint4 beam_load16(const T* p) {
 // Most entries that a wave adds to the list: the lanes above the W-th largest maximum hold all of theirs, the equal ones W.
 constexpr int beam_list_cap(int W, int per_lane) { return (W - 1) * per_lane + W; }
 
+// (six waves on a SIMD: 32 words a lane take 28 us at 16 x 16 x 128000, five waves 30, eight, with spills, 33)
 template <typename T, int NL>
-__global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(const BeamArgs a) {
+__global__ void __launch_bounds__(kBeamThreads, 6) beam_slice_kernel(const BeamArgs a) {
     constexpr int EPV = ElemTraits<T>::kPerVec, NW = kBeamThreads / kWave;
     extern __shared__ __attribute__((aligned(16))) unsigned long long list[];  // what can be among the best, and eight more
     __shared__ float w_max[NW];
