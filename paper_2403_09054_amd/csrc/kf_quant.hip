@@ -1,4 +1,4 @@
-// Caches of 4 bits for gfx950: the decode step's split kernel over them, and the eviction of 16-bit rows into them.
+// Caches of 4 bits for gfx950: the decode step over them, and the eviction of 16-bit rows into them.
 //
 // A row of D elements is D/2 bytes of codes -- E2M1: sign, two exponent bits, one mantissa bit, i.e. 0 1/2 1 3/2 2 3 4 6 --
 // and 16 scale bytes, one for every D/16 elements: a power of two, the smallest with which none of them is above 7 (what
@@ -19,7 +19,6 @@
 #include "kf_merge.h"
 
 namespace kf {
-
 
 constexpr int kQuantThreads = 256;
 constexpr int kQuantWaves = kQuantThreads / kWave;
@@ -50,7 +49,7 @@ __device__ __forceinline__ uint32_t quant_codes(uint32_t w, uint32_t pair, float
 }
 // One group of N = D/16 elements at `src` (16 bits each) -> its codes and scale byte in the row at `dst`.  Magnitudes compare as
 // 15-bit numbers, pair by pair; one conversion instruction makes two codes.  (Element by element in fp32, with the seven borders
-// between codes, the eviction of 512 units of 1024 rows x 128 took 112 us, 87 so, and the step of 16 heads x 1024 x 256 loses 3.2 of its 10.7 us.)
+// between codes, the eviction of 512 units of 1024 rows x 128 took 112 us, 87 so; a step of 16 heads x 1024 x 256 lost 3.2 of 10.7 us.)
 template <typename T, int D>
 __device__ __forceinline__ void quant_group(const char* src, char* dst, int g) {
     constexpr int N = D / 16, P = N / 2;
