@@ -619,7 +619,9 @@ __device__ __forceinline__ void select_unit(const SelectArgs& a, int64_t u) {
 
     // ---- compact: front-to-back gather through registers
     const int PPR = a.row_bytes >> 4;  // 16-byte pieces per row
-    const int rpp = NT / PPR;          // rows per pass of the workgroup
+    // rows per pass of the workgroup; a tile has no more rows than the workgroup has threads, of which each moves the score
+    // and the position of one row (48-byte rows would make 1364)
+    const int rpp = min(NT / PPR, NT / kSelectGroups);
     const int R = rpp * kSelectGroups; // rows per tile
     const int piece = tid % PPR, rsub = tid / PPR;
     uint4* Kb = (uint4*)((char*)a.K + (size_t)u * a.cap * a.row_bytes);

@@ -534,3 +534,43 @@ def test_eviction_from_one_four_bit_cache_into_another():
 def test_units_too_long_for_the_splits_are_refused():
     c = kf.Cache(K=0x10000, V=0x20000, score=0x30000, pos=0x40000, len=0x50000, L=1, B=1, H=1, d=256, cap=300000, dtype=kf.BF16_Q4, q_per_kv=8)
     expect(binding.KF_EUNSUPPORTED, kf.kf_decode_step, c, 0x1000, 0x2000, 0x3000, 10, 0, 1.5, 0.1, seeds=0x4000, out=0x5000, workspace=(0x100000, 1 << 40), stream=0)
+
+
+# Rows of 48 bytes make tiles of more rows than other types' do: several tiles of a unit, and what lies behind the first.
+FAR = [(64, 4000, 1500), (64, 4000, 3000), (64, 9000, 8000), (128, 4000, 3000), (256, 4000, 1500)]  # d, cap, k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,cap,k", FAR)
+def test_eviction_in_place_of_units_longer_than_a_tile(d, cap, k):
+    B, H, w = 2, 4, 33
+    p = Pair(71 + d, 1, B, H, d, cap, kf.F16_Q4, fill=cap)
+    lens = np.array([k - 5, k, k + 1, k + 2, cap, cap - 1, (k + cap) // 2, cap - 77], np.int32).reshape(1, B, H)
+    p.oc.len[...] = lens
+    p.gc.len.copy_(torch.from_numpy(lens))
+    p.oc.score[0, 0, 3, 0], p.oc.score[0, 1, 0, 3] = 0.0, 0.0  # rows move from the first slots on
+    p.gc.score.copy_(torch.from_numpy(p.oc.score))
+    ref = p.oc.select_evict(k, w)
+    assert (ref[0, 1, 0, :8] != np.arange(8)).any()
+    kept = torch.zeros((1, B, H, k), dtype=torch.int32, device="cuda")
+    kf.kf_select_evict(p.gc, k, w, kept, p.ws)
+    np.testing.assert_array_equal(host(kept), ref)
+    p.same("evict")
+    assert error_word(p.ws) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,cap,k", FAR)
+def test_steps_of_units_longer_than_a_tile_and_far_over_budget(d, cap, k):
+    B, H, w = 2, 4, 33
+    p = Pair(73 + d, 1, B, H, d, cap, kf.BF16_Q4, fill=cap - 1)
+    lens = np.array([k - 5, k - 1, k, k + 1, cap - 1, cap - 2, (k + cap) // 2, cap - 77], np.int32).reshape(1, B, H)
+    p.oc.len[...] = lens
+    p.gc.len.copy_(torch.from_numpy(lens))
+    q, kn, vn = p.token()
+    want = p.oracle(q, kn, vn, p.first, 1.5, ko.NOISE_GUMBEL)
+    p.oc.select_evict(k, w)
+    kf.kf_decode_select_step(p.gc, *p.gpu_args(q, kn, vn), p.first, 0, 1.5, p.scale, kf.NOISE_GUMBEL, dev(p.seeds), None, p.out, k=k, w=w, workspace=p.ws)
+    assert error_word(p.ws) == 0
+    assert_close_out(host(p.out), want)
+    p.same("step")
