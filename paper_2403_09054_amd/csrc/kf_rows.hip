@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const RowsArgs a) {
     int nb = a.n;
     if (a.seq_n) {
         nb = a.seq_n[b];
-        if (nb > a.n) nb = 0;  // no such length: the sequence is left out
+        if (nb < 1 || nb > a.n) nb = 0;  // no such length: the sequence is left out (and nb - t0 does not leave its range)
     }
     const int cnt = min(1 << a.tt_shift, nb - t0);
     if (cnt <= 0) return;

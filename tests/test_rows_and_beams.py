@@ -420,3 +420,24 @@ def test_rows_and_beams_on_a_stream_of_their_own():
         stream.synchronize()
         got.append([Q, *out, new])
     assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [9, 70])
+def test_rows_of_any_length_that_is_none_are_left_out(n):
+    """Also lengths from which a later tile's first token cannot be taken away in 32 bits."""
+    g = torch.Generator().manual_seed(6)
+    low = -2 ** 31
+    lens = torch.tensor([n, low, low + 7, low + n, -n, 2 ** 31 - 1, 1], dtype=torch.int32).cuda()
+    B, H, d, room = len(lens), 2, 64, 16  # (rows behind a sequence's, as a padded batch has them)
+    x = [torch.randn((B, n + room, H, d), generator=g).half().cuda() for _ in range(3)]
+    Q = torch.full((B, H, n, d), 3.0, dtype=torch.float16, device="cuda")
+    K, V = (torch.full((B, H, n + room, d), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    st = x[0].stride()[:2]
+    kf.kf_norm_rotate(kf.Rows(B=B, n=n, H=H, d=d, dtype=kf.F16, kv_rows=n + room, q_stride=st, k_stride=st, v_stride=st, seq_n=lens), *x, Q, K, V)
+    torch.cuda.synchronize()
+    for got, src in zip((Q, K, V), x):
+        want = torch.full_like(got, 3.0)
+        for b, m in ((0, n), (B - 1, 1)):
+            want[b, :, :m] = src[b, :m].transpose(0, 1)
+        assert torch.equal(got, want)
