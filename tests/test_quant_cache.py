@@ -574,3 +574,20 @@ def test_steps_of_units_longer_than_a_tile_and_far_over_budget(d, cap, k):
     assert error_word(p.ws) == 0
     assert_close_out(host(p.out), want)
     p.same("step")
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_packed_again_from_what_they_stand_for_are_the_same(d):
+    """A group's largest element is above 7/2 of its unit and becomes 4 or 6 of them, so the exponent comes back."""
+    rng = np.random.default_rng(d)
+    for dt in (torch.bfloat16, torch.float16):
+        x = values(rng, (60, d), dt).float().numpy()
+        x[1], x[2], x[3, ::2] = 0.0, -0.0, 0.0
+        x[4] = rng.integers(-28, 29, d) * 0.25           # whole and half steps: ties
+        x[5] = np.linspace(3.5, 7.0, d)
+        x[6] = np.where(np.arange(d) % 2, 1.0, -1.0) * float(torch.finfo(dt).max)
+        x[7] = float(torch.finfo(dt).tiny) * 0.75
+        x[20:40] *= 2.0 ** rng.integers(-12, 9, (20, 1))
+        rows = pack(x)
+        assert not np.isnan(unpack(rows)).any()
+        np.testing.assert_array_equal(pack(unpack(rows)), rows)
