@@ -643,8 +643,11 @@ hipError_t launch_quant_gather(const GatherArgs& g, int32_t d, int32_t dtype, hi
 static int quant_rpb(int32_t d, int32_t G) { return kWave / (d / quant_epl(G)) * kQuantWaves; }
 static size_t quant_lds(int32_t G, int64_t chunk, int32_t d) { return (size_t)((2 * G + (G > 1 ? 1 : 0)) * (chunk + 1) + kQuantWaves * G * d) * sizeof(float); }
 
-// Most splits of a unit of up to m tokens (what the records are sized for): as many as keep two rounds of rows for each, up
-// to 2048 workgroups in all, and as many as the logits in LDS ask for.
+// Fewest and most splits of a unit of so many rows (the records are sized for the most): as many as the logits in LDS ask for, and
+// as many as keep two rounds of rows for each, up to 2048 workgroups in all and 63 more than the fewest.  That bound is for few long units: the
+// model below knows no price of a split in the merge, and would take 100 to 256 there, which lose (slot layout, best split / with the bound / without):
+// 1 unit x 32000 x 128, 8 heads 48 splits 45 us, 91 51, 250 87; 2 x 32768 x 256, 8 heads 48 67, 108 89, 256 166; 4 x 16384 x 128, 4 heads
+// 47 30, 64 32, 256 58; 1 x 40000 x 128 90 25, 70 26, 209 29; 8 x 40000 x 128 63 34, 63 34, 125 37.
 static void quant_split_range(int64_t U, int64_t rows, int32_t d, int32_t G, int64_t* lo, int64_t* hi) {
     const int64_t rpb = quant_rpb(d, G);
     const int64_t fit = (int64_t)((kQuantLds / sizeof(float) - (size_t)kQuantWaves * G * d) / (2 * G + 1) - 1) / rpb * rpb;
@@ -653,6 +656,7 @@ static void quant_split_range(int64_t U, int64_t rows, int32_t d, int32_t G, int
     const int64_t most = (2048 + U - 1) / U;
     if (*hi > most) *hi = most;
     if (*hi > kDecodeMaxSplits) *hi = kDecodeMaxSplits;
+    if (*hi > *lo + 63) *hi = *lo + 63;
     if (*hi < *lo) *hi = *lo;
 }
 int32_t quant_max_splits(int64_t U, int32_t m, int32_t d, int32_t G) {
@@ -667,12 +671,14 @@ DecodePlan plan_quant(int64_t U, int32_t m, int32_t d, int32_t G) {
     quant_split_range(U, rows, d, G, &lo, &hi);
     // A launch runs in rounds of as many workgroups as fit (registers: 16 waves on a compute unit; LDS); one of r workgroups on a
     // compute unit takes its chain of trips to memory and a time by its rows that falls short of proportion for small
-    // r; splits add the launch that merges them.  In microseconds, fitted to the shapes below, best split and the next:
-    // 2048 units x 1024 x 128 1 split 75, 2 105, 4 123; 256 x 4096 x 128, 2 heads 4 splits 57, 2 64, 1 91; 512 x 2048 x 128, 4 heads
-    // 4 splits 71, 2 76; 128 x 4000 x 128 8 splits 31, 4 34, 2 41; 16 x 1024 x 256 6 splits 17.4, 16 18, 2 23.
+    // r; splits add the launch that merges them.  Slot layout, replayed graphs, microseconds (the one taken first): 256 units x 4096 x 128,
+    // 2 heads 4 splits 57, 2 62, 8 60; 512 x 2048 x 128, 4 heads 4 72, 3 70, 2 76; 128 x 4000 x 128 8 32, 4 32, 2 41; 16 x 1024 x 256 16
+    // 14.6, 8 14.3, 2 19.5; 448 x 1024 x 256 1 38, 2 42.  Where the model falls short: few short units, whose one workgroup it takes to
+    // be cheaper than it is (32 x 1024 x 128 1 18.3, 6 14.0; 64 x 2048 x 64 1 25.5, 6 16.7), and few units with 4 or 8 heads (8 x 5000 x
+    // 128, 4 heads 53 27.5, 23 24.1; 64 x 300 x 256, 8 heads 7 25.6, 4 21.4).
     const double fixed = 6.0, row = (G == 1 ? 3.4e-5 : G == 2 ? 4e-5 : G == 4 ? 5.6e-5 : 1.1e-4) * (d / 2 + 16);
     double best = 0.0;
-    for (int64_t S = lo; S <= hi && S <= lo + 63; ++S) {
+    for (int64_t S = lo; S <= hi; ++S) {
         const int64_t chunk = ((rows + S - 1) / S + rpb - 1) / rpb * rpb, n = (rows + chunk - 1) / chunk;
         const size_t lds = quant_lds(G, chunk, d);
         if (lds > kQuantLds) continue;

@@ -591,3 +591,14 @@ def test_rows_packed_again_from_what_they_stand_for_are_the_same(d):
         rows = pack(x)
         assert not np.isnan(unpack(rows)).any()
         np.testing.assert_array_equal(pack(unpack(rows)), rows)
+
+
+@pytest.mark.parametrize("U,cap,d,G", [(1, 32001, 128, 8), (1, 40001, 128, 1), (2, 32769, 256, 8), (4, 16385, 128, 4)])
+def test_the_workspace_holds_the_splits_that_are_taken(U, cap, d, G):
+    """Few long units: records for the most splits that any length takes, within a quarter, and no more."""
+    c = kf.Cache(K=0x10000, V=0x20000, score=0x30000, pos=0x40000, len=0x50000, L=1, B=1, H=U, d=d, cap=cap, dtype=kf.BF16_Q4, q_per_kv=G)
+    most = max(kf.kf_decode_launch_shape(c, m)[0] for m in {*range(1, cap, 97), cap})
+    records = U * most * G * (d + 4) * 4
+    # increments and survivors; then, of the ordered eviction, an entry for every 227 rows at least; slices and roundings
+    rest = U * cap * 4 * (G + 1) + U * (cap // 227 + 1) * (2 * (d // 2 + 16) + 8) + U * 16 * 12 + 16 * 256
+    assert records <= kf.kf_workspace_bytes(c) <= records * 5 // 4 + rest
