@@ -56,7 +56,9 @@ typedef enum {
      * to 6.  A group that holds an infinity or a NaN has byte 255 and stands for NaNs.
      * Served by every call on a cache but kf_prefill_score: a prompt is staged and scored in 16 bits and its survivors
      * move into the 4-bit cache by kf_select_evict_into.  In a step, the new token's own key and value take part as
-     * they are given; from the next step on as they are held. */
+     * they are given; from the next step on as they are held.  A step takes units of up to 180225 tokens with 8 query heads
+     * per cached head (d = 128: 237569, d = 64: 262145), 454657 with 4, 925697 with 2 and 1630209 with 1; an m_hint above
+     * that, or a cap above it without one, is refused (KF_EUNSUPPORTED). */
     KF_BF16_Q4 = 17,
     KF_F16_Q4 = 18
 } kf_dtype;

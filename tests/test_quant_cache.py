@@ -602,3 +602,21 @@ def test_the_workspace_holds_the_splits_that_are_taken(U, cap, d, G):
     # increments and survivors; then, of the ordered eviction, an entry for every 227 rows at least; slices and roundings
     rest = U * cap * 4 * (G + 1) + U * (cap // 227 + 1) * (2 * (d // 2 + 16) + 8) + U * 16 * 12 + 16 * 256
     assert records <= kf.kf_workspace_bytes(c) <= records * 5 // 4 + rest
+
+
+LONGEST = {(64, 8): 262145, (128, 8): 237569, (256, 8): 180225, (256, 4): 454657, (256, 2): 925697, (256, 1): 1630209}  # d, query heads
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_the_longest_units_of_a_step_are_those_of_the_documentation(d, G):
+    longest = LONGEST.get((d, G), LONGEST[256, G])
+    c = kf.Cache(K=0x10000, V=0x20000, score=0x30000, pos=0x40000, len=0x50000, L=1, B=1, H=1, d=d, cap=2500000, dtype=kf.BF16_Q4, q_per_kv=G)
+    for m in (longest, longest - 1, longest // 2):
+        S, chunk = kf.kf_decode_launch_shape(c, m)
+        assert S <= 256 and S * chunk >= m - 1
+    if (d, G) in LONGEST:
+        assert kf.kf_decode_launch_shape(c, longest + 1)[0] > 256
+        for hint in (longest + 1, 0):  # (0: the whole capacity)
+            expect(binding.KF_EUNSUPPORTED, kf.kf_decode_step, c, 0x1000, 0x2000, 0x3000, 10, hint, 1.5, 0.1, seeds=0x4000, out=0x5000,
+                   workspace=(0x100000, 1 << 40), stream=0)
