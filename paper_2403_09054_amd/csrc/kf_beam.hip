@@ -10,9 +10,11 @@
 //            keys cuts all four lists.
 //   request  a workgroup takes a request: each row's slices are joined (statistics in 64 bits, lists by taking their
 //            smallest heads), then the rows' lists, totals in 64 bits; then the rows are numbered.
-// What bounds the first launch is its instructions, 700 to 900 a wave for 2048 words (64 x 4 rows x 50304 in fp32 16 us, 3.2 TB/s;
-// 16 x 16 x 128000 in halves, a fifth of the rows ended, 28 us), the second a chain of short steps, W picks a row, then W
-// picks (4 beams 5.5 us, 16 beams 13.6).
+// The first launch (64 x 4 rows x 50304 in fp32 16 us, 3.2 TB/s; 16 x 16 x 128000 in halves, a fifth of the rows ended, 28 us) is
+// bound by no one thing: its instructions, 700 to 900 a wave for 2048 words, are 6 to 10 of the 16 us, a trip to memory, the search's and the
+// reductions' chains and the waves' starts the rest.  It grows by 1 us for 220 workgroups, also where the next round of them begins, and a
+// row's last slice costs as much with one word as with 8192 (256 rows x 49152 18.8 us for both launches, x 49153 21.1).  What
+// bounds the second is a chain of short steps, W picks a row, then W picks (4 beams 5.5 us, 16 beams 13.6).
 #include "kf_device.h"
 #include "kf_internal.h"
 

@@ -12,7 +12,9 @@
 // elements of a row (16 bytes of codes, or 8 where several query heads need the registers).  The new token's own key and value
 // enter as they were given, in 16 bits.  With a quarter to a third of the bytes of 16-bit rows the launch is close to being bound by
 // its instructions as well as by bytes.  Steps in the slot layout, one launch: 2048 units x 1024 x 128 75 us (4.9 TB/s of rows, scores and
-// positions), 2048 x 2048 x 128 139 us (5.2 TB/s); with 4 query heads 512 x 2048 x 128 71 us (2.6 TB/s).  Non-temporal loads lose 20 %
+// positions), 2048 x 2048 x 128 139 us (5.2 TB/s); with 4 query heads 512 x 2048 x 128 71 us (2.6 TB/s).  Few units gain nothing by 4 bits:
+// their chains of trips are as long, and 16-bit rows have a form for them that these have not (slot layout, 16 bits / 4 bits, replayed: 16 x
+// 1024 x 256 14.9 / 13.9 us, 64 x 1024 x 128 16.3 / 17.8, 512 x 1024 x 128 48 / 30; ordered 13.3 / 18.6, 18.8 / 23.3, 78 / 43).  Non-temporal loads lose 20 %
 // here: a cache line holds pieces of two rows' codes and scales, and is asked for more than once.
 #include "kf_device.h"
 #include "kf_internal.h"
