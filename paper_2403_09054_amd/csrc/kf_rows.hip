@@ -8,8 +8,8 @@
 // with (a, b) = elements (2i, 2i+1) or (i, i + rot/2) of a row.  Everything is computed in 32 bits and rounded once, when the
 // row is stored; the angle's turns are counted in 64 bits, so that a position of 100 000 costs no accuracy.
 //
-// What bounds it is bytes: each row is read and written once (8 x 4096 tokens x 96 heads x 128, padded: 1.0 GB in 225 to 246 us on
-// three cards, 4.1 to 4.5 TB/s; a large copy runs at 4.7).  One token a sequence is bound by a chain: positions and frequencies, the
+// What bounds it is bytes: each row is read and written once (8 x 4096 tokens x 96 heads x 128, padded: 1.0 GB in 222 to 246 us on
+// four cards, 4.1 to 4.5 TB/s; a large copy runs at 4.7).  One token a sequence is bound by a chain: positions and frequencies, the
 // angles, then the rows' own trip to memory, which waits for them although no address asks for it (64 sequences x 96 heads x 128
 // 5.0 us).  A lane takes 16 bytes of a row, d * sizeof(T) / 16 adjacent lanes a row.  A workgroup takes `tt` neighbouring
 // tokens of one sequence and `hc` heads: the cosines and sines of its tokens are formed once, in LDS, for all its heads.
