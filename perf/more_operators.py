@@ -318,7 +318,8 @@ def _own_prompt(kf, s):
             o = s["out"].stride()
             s["cfg"] = kf.Prompt(seq_n=s["seq_n"], seq_m=s["seq_m"], q_stride=s["Q"].stride()[:3], k_stride=s["K"].stride()[:3],
                                  v_stride=s["V"].stride()[:3], out_stride=(o[0], o[2], o[1]), **of)
-    kf.kf_prompt_attend(s["cfg"], s["Q"], s["K"], s["V"], s["out"])
+        s["ws"] = kf.new_prompt_workspace(s["cfg"])
+    kf.kf_prompt_attend(s["cfg"], s["Q"], s["K"], s["V"], s["out"], workspace=s["ws"])
     return s["out"]
 
 
