@@ -423,6 +423,105 @@ kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *sco
                          int32_t *parent, int32_t *token, float *new_score, int32_t *new_done, int32_t *rank,
                          void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Attention over prompts, which kf_prefill_score scores but does not attend: for every sequence b, head and query row i of nq
+ *     x_ij = scale*<Q_i, K_j> - slope_h*(p_i - j)      j <= p_i = i + nk - nq  (the last query is the last key's)
+ *     out_i = sum_j softmax_j(x_i)_j V_j
+ * over the sequence's nk keys: a whole prompt (nk = nq), or the last rows of one whose earlier keys are there.  A row that sees no
+ * key (nq > nk), or whose logits are all minus infinity, is zero.  What a row does not see does not reach it, whatever it holds.
+ * Logits, softmax and sums have 32 bits; with 16-bit elements the probabilities are rounded to the element type for their
+ * product with V.  A row of out is rounded once.
+ *   strides : elements between sequences, heads, tokens; all three zero: Q [B][H*q_per_kv][n][d], K and V [B][H][m][d] (a layer of a
+ *             cache with cap = m), out [B][n][H*q_per_kv][d]; of packed rows: [tokens][heads][d]
+ *   q_start, k_start : DEVICE [B+1] or NULL.  Packed sequences: b's rows are tokens start[b] .. start[b+1]-1 of one list (the
+ *             stride between sequences is not used); q_start is that of Q and out, k_start of K and V
+ *   seq_n, seq_m : DEVICE [B] or NULL.  Padded sequences: b has seq_n[b] of n rows, seq_m[b] of m keys.  Not together with
+ *             the start of the same rows.  Rows behind a sequence are neither read nor written.
+ * n and m bound a sequence's rows and keys; one whose rows lie outside [1, n] or whose keys lie outside [0, m] is left out.
+ * Any q_per_kv is served.  out must not overlap the inputs.  The workspace (kf_prompt_workspace_bytes) needs no initial contents.
+ * Errors: KF_EINVAL for sizes, null pointers, scale not finite, alignment (pointers and strides: 16 bytes), seq_n with q_start, seq_m
+ * with k_start; KF_EUNSUPPORTED for a dtype / d pair that is not built; KF_EWORKSPACE.
+ */
+typedef struct {
+    int32_t B, n, m, H, q_per_kv, d, dtype; /* q_per_kv 0 means 1 */
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+    const int32_t *q_start, *k_start;
+    const int32_t *seq_n, *seq_m;
+    float scale;
+    const float *alibi_slopes;              /* DEVICE [H*q_per_kv] or NULL */
+} kf_prompt;
+size_t kf_prompt_workspace_bytes(const kf_prompt *p);
+kf_status kf_prompt_attend(const kf_prompt *p, const void *Q, const void *K, const void *V, void *out, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * A cache of 8 bits in pages, for sequences that keep all their tokens or share a prompt (the caches above hold what a budget leaves,
+ * one row of the batch each).  A page is KF_PAGE_TOKENS tokens of every layer and cached head.  Codes are E4M3 (sign, 4 bits of
+ * exponent, 3 of mantissa; largest 448, 0x7F is no number), multiplied by one power of two for each page, head and tensor: the
+ * smallest of 2^-117 .. 2^119 with which no finite element of the page's rows is above 448, each element rounded to the nearest
+ * code, ties to the even one (a bf16 above 448 * 2^119 to that).  An infinity or a NaN is held as 0x7F.  A row that needs a larger scale than its page has makes the
+ * page's older codes be rounded again.
+ *   K       : DEVICE [L][pages][H][KF_PAGE_TOKENS][d] key codes, 16-byte aligned
+ *   V       : DEVICE [L][pages][H][d][KF_PAGE_TOKENS] value codes, 16-byte aligned
+ *   k_scale, v_scale : DEVICE [L][pages][H]
+ *   table   : DEVICE [B][max_pages] page numbers of a sequence's tokens, in order; -1 behind them.  All -1 at first.
+ *   len     : DEVICE [B] tokens of each sequence.  Zero at first.
+ *   refs    : DEVICE [pages] sequences that hold a page; 0: free.  Zero at first.
+ * Sequences share full pages only; a last page that is not full is its sequence's alone, so that no row is written to a shared page.
+ * Pages are taken lowest number first, sequences in order.  table, len and refs serve all layers; a caller that runs its layers one
+ * after the other passes the struct with L = 1 and the layer's K, V and scales to kf_page_write and kf_page_step.
+ * dtype (KF_BF16 or KF_F16) is that of the rows that go in and of the queries.  d: 64, 128 or 256; q_per_kv: 1, 2, 4 or 8; B up to 8192.
+ * The workspace (kf_page_workspace_bytes, by the whole struct or one layer of it) is DEVICE memory, 16-byte aligned; only its first
+ * word must start as zero: it counts sequences, or pages of a unit, that a kernel had to leave out.
+ */
+#define KF_PAGE_TOKENS 64
+typedef struct {
+    void *K, *V;
+    float *k_scale, *v_scale;
+    int32_t *table, *len, *refs;
+    int32_t L, B, H, d, pages, max_pages, dtype, q_per_kv;
+} kf_pages;
+size_t kf_page_workspace_bytes(const kf_pages *p);
+
+/* Room for n more tokens of every sequence, or seq_n[b] of them (DEVICE [B] or NULL; one outside [1, n] leaves its sequence as it
+ * is): len grows by them, and pages are taken as they need.  A sequence for which the table or the free pages do not suffice is
+ * left as it is and counted; the ones behind it may still find room.  The rows themselves are then written by kf_page_write or
+ * kf_page_step, layer by layer. */
+kf_status kf_page_reserve(const kf_pages *p, int32_t n, const int32_t *seq_n, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The rows of the last n (or seq_n[b]) tokens of every sequence, as just reserved: k and v are DEVICE [L][B][H][rows][d], rows [0, n)
+ * or [0, seq_n[b]) of each head are read (rows >= n; 0 means n).  A sequence that holds fewer tokens than that is left out and counted. */
+kf_status kf_page_write(const kf_pages *p, const void *k, const void *v, int32_t n, int32_t rows, const int32_t *seq_n, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* One token of every sequence, reserved before: attention over its len tokens, the last of which is k_new, v_new, and its row written.
+ *     x_j = scale*<q, K_j> - slope_h*(len-1 - j),  out = sum_j softmax(x)_j V_j
+ * As in a step on a 4-bit cache, the token's own key and value take part as they are given, from the next step on as they are held.
+ * q is DEVICE [L][B][H*q_per_kv][d], k_new and v_new [L][B][H][d], out [L][B][H*q_per_kv][d] fp32.  Positions are places in the
+ * cache.  m_hint bounds len (0: max_pages * KF_PAGE_TOKENS) and only shapes the launch.  With seq_n (DEVICE [B] or NULL) a sequence
+ * whose seq_n[b] is not 1 takes no step: its out is zero and nothing of it is written.  One that takes a step with no token, or more
+ * than its row of the table has room for, gets zeros too and is counted; a page number outside [0, pages) leaves its tokens out. */
+kf_status kf_page_step(const kf_pages *p, const void *q, const void *k_new, const void *v_new, float scale, const float *alibi_slopes,
+                       const int32_t *seq_n, int32_t m_hint, float *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Row b goes on as row parent[b] does (DEVICE [B], as kf_beam_select writes it and kf_beam_fork takes it: parent[parent[b]] ==
+ * parent[b]).  For every b with parent[b] != b its pages are released, the parent's full pages shared, its last page copied if it is not
+ * full.  A parent out of range or one that does not continue itself leaves the row as it is and is counted; a row for whose last page
+ * none is free, or whose parent's row of the table is no such, comes out empty and is counted. */
+kf_status kf_page_fork(const kf_pages *p, const int32_t *parent, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Releases the pages of the sequences with which[b] != 0 (DEVICE [B]; NULL: all); they are empty then. */
+kf_status kf_page_free(const kf_pages *p, const int32_t *which, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Every sequence of more than k tokens with which[b] != 0 (DEVICE [B]; NULL: all) keeps k of them: head h of layer l keeps the
+ * tokens keep[l][b][h][0..k) (DEVICE [L][B][H][k], in the order in which they are to stand, as kf_select_evict writes kept_idx for a
+ * cache that holds the same tokens).  The kept rows move into new pages, with the scale that these rows ask for, and the old pages are
+ * released: ceil(k / KF_PAGE_TOKENS) free pages are needed for each such sequence before its own become free.  A sequence for which
+ * there are none, or whose row of the table names a page that there is not, is left as it is and counted; a token outside [0, len) is
+ * replaced by zeros and counted.  All layers must be in the struct. */
+kf_status kf_page_compact(const kf_pages *p, const int32_t *keep, int32_t k, const int32_t *which, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

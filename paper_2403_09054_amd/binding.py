@@ -26,7 +26,10 @@ KF_OK, KF_EINVAL, KF_EUNSUPPORTED, KF_EWORKSPACE, KF_EDEVICE = 0, -1, -2, -3, -4
 SYMBOLS = ("kf_version", "kf_last_error", "kf_tau", "kf_noise_bits", "kf_workspace_bytes",
            "kf_prefill_score", "kf_decode_step", "kf_select_evict", "kf_select_evict_into", "kf_decode_select_step",
            "kf_decode_launch_shape", "kf_decode_select_step_at", "kf_beam_fork", "kf_decode_select_step_noalloc",
-           "kf_norm_rotate", "kf_beam_workspace_bytes", "kf_beam_select")
+           "kf_norm_rotate", "kf_beam_workspace_bytes", "kf_beam_select", "kf_prompt_workspace_bytes", "kf_prompt_attend",
+           "kf_page_workspace_bytes", "kf_page_reserve", "kf_page_write", "kf_page_step", "kf_page_fork", "kf_page_free",
+           "kf_page_compact")
+PAGE_TOKENS = 64
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -65,6 +68,19 @@ class kf_rows(C.Structure):
 class kf_beams(C.Structure):
     _fields_ = [("R", C.c_int32), ("W", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("row_stride", C.c_int64),
                 ("eos", C.c_int32)]
+
+
+class kf_prompt(C.Structure):
+    _fields_ = [("B", C.c_int32), ("n", C.c_int32), ("m", C.c_int32), ("H", C.c_int32), ("q_per_kv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("out_stride", C.c_int64 * 3), ("q_start", C.c_void_p), ("k_start", C.c_void_p), ("seq_n", C.c_void_p),
+                ("seq_m", C.c_void_p), ("scale", C.c_float), ("alibi_slopes", C.c_void_p)]
+
+
+class kf_pages(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("table", C.c_void_p),
+                ("len", C.c_void_p), ("refs", C.c_void_p), ("L", C.c_int32), ("B", C.c_int32), ("H", C.c_int32), ("d", C.c_int32),
+                ("pages", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32), ("q_per_kv", C.c_int32)]
 
 
 _lib = None
@@ -128,6 +144,24 @@ def lib():
         L.kf_beam_workspace_bytes.argtypes = [C.POINTER(kf_beams)]
         L.kf_beam_select.restype = C.c_int
         L.kf_beam_select.argtypes = [C.POINTER(kf_beams), vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.kf_prompt_workspace_bytes.restype = C.c_size_t
+        L.kf_prompt_workspace_bytes.argtypes = [C.POINTER(kf_prompt)]
+        L.kf_prompt_attend.restype = C.c_int
+        L.kf_prompt_attend.argtypes = [C.POINTER(kf_prompt), vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.kf_page_workspace_bytes.restype = C.c_size_t
+        L.kf_page_workspace_bytes.argtypes = [C.POINTER(kf_pages)]
+        L.kf_page_reserve.restype = C.c_int
+        L.kf_page_reserve.argtypes = [C.POINTER(kf_pages), C.c_int32, vp, vp, C.c_size_t, vp]
+        L.kf_page_write.restype = C.c_int
+        L.kf_page_write.argtypes = [C.POINTER(kf_pages), vp, vp, C.c_int32, C.c_int32, vp, vp, C.c_size_t, vp]
+        L.kf_page_step.restype = C.c_int
+        L.kf_page_step.argtypes = [C.POINTER(kf_pages), vp, vp, vp, C.c_float, vp, vp, C.c_int32, vp, vp, C.c_size_t, vp]
+        L.kf_page_fork.restype = C.c_int
+        L.kf_page_fork.argtypes = [C.POINTER(kf_pages), vp, vp, C.c_size_t, vp]
+        L.kf_page_free.restype = C.c_int
+        L.kf_page_free.argtypes = [C.POINTER(kf_pages), vp, vp, C.c_size_t, vp]
+        L.kf_page_compact.restype = C.c_int
+        L.kf_page_compact.argtypes = [C.POINTER(kf_pages), vp, C.c_int32, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -400,3 +434,155 @@ def kf_beam_select(beams: Beams, logits, score, parent, token, new_score, done=N
     wp, wb = _ws(workspace)
     _check(lib().kf_beam_select(C.byref(cs), _ptr(logits), _ptr(score), _ptr(done), _ptr(parent), _ptr(token), _ptr(new_score),
                                 _ptr(new_done), _ptr(rank), wp, wb, _stream(stream)))
+
+
+@dataclass
+class Prompt:
+    """Sizes and layout of an attention over prompts (kf_prompt_attend).  Strides: elements between sequences, heads and
+    tokens, (0, 0, 0) for contiguous rows; q_start, k_start: int32 [B+1], packed sequences; seq_n, seq_m: int32 [B],
+    padded ones; slopes: float32 [H * q_per_kv]; any of these may be None."""
+    B: int
+    n: int                 # query rows of a sequence, at most
+    m: int                 # keys of a sequence, at most
+    H: int
+    d: int
+    dtype: int
+    scale: float
+    q_per_kv: int = 1
+    q_stride: tuple = (0, 0, 0)
+    k_stride: tuple = (0, 0, 0)
+    v_stride: tuple = (0, 0, 0)
+    out_stride: tuple = (0, 0, 0)
+    q_start: object = None
+    k_start: object = None
+    seq_n: object = None
+    seq_m: object = None
+    slopes: object = None
+
+    def c_struct(self) -> kf_prompt:
+        three = C.c_int64 * 3
+        return kf_prompt(self.B, self.n, self.m, self.H, self.q_per_kv, self.d, self.dtype, three(*self.q_stride), three(*self.k_stride),
+                         three(*self.v_stride), three(*self.out_stride), _ptr(self.q_start), _ptr(self.k_start), _ptr(self.seq_n),
+                         _ptr(self.seq_m), self.scale, _ptr(self.slopes))
+
+
+def kf_prompt_workspace_bytes(prompt: Prompt) -> int:
+    cs = prompt.c_struct()
+    return int(lib().kf_prompt_workspace_bytes(C.byref(cs)))
+
+
+def new_prompt_workspace(prompt: Prompt, device="cuda"):
+    """A workspace tensor for kf_prompt_attend with these sizes."""
+    import torch
+    nbytes = kf_prompt_workspace_bytes(prompt)
+    if nbytes == 0:
+        raise KeyformerError(KF_EUNSUPPORTED, lib().kf_last_error().decode())
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def kf_prompt_attend(prompt: Prompt, Q, K, V, out, workspace=None, stream=None) -> None:
+    """Q [B,H*q_per_kv,n,d], K, V [B,H,m,d], out [B,n,H*q_per_kv,d], or as the strides say."""
+    cs = prompt.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_prompt_attend(C.byref(cs), _ptr(Q), _ptr(K), _ptr(V), _ptr(out), wp, wb, _stream(stream)))
+
+
+@dataclass
+class Pages:
+    """Torch tensors that back a kf_pages.  K uint8 [L,pages,H,64,d], V uint8 [L,pages,H,d,64] (torch.float8_e4m3fn codes);
+    k_scale, v_scale float32 [L,pages,H]; table int32 [B,max_pages]; len int32 [B]; refs int32 [pages]."""
+    K: object
+    V: object
+    k_scale: object
+    v_scale: object
+    table: object
+    len: object
+    refs: object
+    L: int
+    B: int
+    H: int
+    d: int
+    pages: int
+    max_pages: int
+    dtype: int
+    q_per_kv: int = 1
+
+    @staticmethod
+    def allocate(L, B, H, d, pages, max_pages, dtype=BF16, device="cuda", q_per_kv=1):
+        import torch
+        return Pages(K=torch.zeros((L, pages, H, PAGE_TOKENS, d), dtype=torch.uint8, device=device),
+                     V=torch.zeros((L, pages, H, d, PAGE_TOKENS), dtype=torch.uint8, device=device),
+                     k_scale=torch.ones((L, pages, H), dtype=torch.float32, device=device),
+                     v_scale=torch.ones((L, pages, H), dtype=torch.float32, device=device),
+                     table=torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+                     len=torch.zeros(B, dtype=torch.int32, device=device), refs=torch.zeros(pages, dtype=torch.int32, device=device),
+                     L=L, B=B, H=H, d=d, pages=pages, max_pages=max_pages, dtype=dtype, q_per_kv=q_per_kv)
+
+    def layer(self, l: int) -> "Pages":
+        """One layer, for callers that write and step their layers one after the other; table, len and refs are shared."""
+        return Pages(K=self.K[l:l + 1], V=self.V[l:l + 1], k_scale=self.k_scale[l:l + 1], v_scale=self.v_scale[l:l + 1], table=self.table,
+                     len=self.len, refs=self.refs, L=1, B=self.B, H=self.H, d=self.d, pages=self.pages, max_pages=self.max_pages,
+                     dtype=self.dtype, q_per_kv=self.q_per_kv)
+
+    def c_struct(self) -> kf_pages:
+        return kf_pages(_ptr(self.K), _ptr(self.V), _ptr(self.k_scale), _ptr(self.v_scale), _ptr(self.table), _ptr(self.len),
+                        _ptr(self.refs), self.L, self.B, self.H, self.d, self.pages, self.max_pages, self.dtype, self.q_per_kv)
+
+
+def kf_page_workspace_bytes(pages: Pages) -> int:
+    cs = pages.c_struct()
+    return int(lib().kf_page_workspace_bytes(C.byref(cs)))
+
+
+def new_page_workspace(pages: Pages, device="cuda"):
+    """A zero-filled workspace tensor for every call on these pages."""
+    import torch
+    nbytes = kf_page_workspace_bytes(pages)
+    if nbytes == 0:
+        raise KeyformerError(KF_EUNSUPPORTED, lib().kf_last_error().decode())
+    return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+
+
+def kf_page_reserve(pages: Pages, n: int = 1, seq_n=None, workspace=None, stream=None) -> None:
+    """seq_n: int32 [B] of new tokens of each sequence (up to n), or None: n for all."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_reserve(C.byref(cs), n, _ptr(seq_n), wp, wb, _stream(stream)))
+
+
+def kf_page_write(pages: Pages, k, v, n: int, rows: int = 0, seq_n=None, workspace=None, stream=None) -> None:
+    """k, v [L,B,H,rows,d]: the rows of the last n (or seq_n[b]) tokens of each sequence; rows: 0 for n."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_write(C.byref(cs), _ptr(k), _ptr(v), n, rows, _ptr(seq_n), wp, wb, _stream(stream)))
+
+
+def kf_page_step(pages: Pages, q, k_new, v_new, scale: float, out, m_hint: int = 0, slopes=None, seq_n=None, workspace=None,
+                 stream=None) -> None:
+    """q [L,B,H*q_per_kv,d], k_new, v_new [L,B,H,d], out float32 [L,B,H*q_per_kv,d]; seq_n: int32 [B], 1 for each sequence that
+    takes the step, or None: all."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_step(C.byref(cs), _ptr(q), _ptr(k_new), _ptr(v_new), scale, _ptr(slopes), _ptr(seq_n), m_hint, _ptr(out), wp, wb,
+                              _stream(stream)))
+
+
+def kf_page_fork(pages: Pages, parent, workspace=None, stream=None) -> None:
+    """parent: int32 [B]; row b of the batch goes on as row parent[b] does."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_fork(C.byref(cs), _ptr(parent), wp, wb, _stream(stream)))
+
+
+def kf_page_free(pages: Pages, which=None, workspace=None, stream=None) -> None:
+    """which: int32 [B], not 0 for each sequence that ends, or None: all."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_free(C.byref(cs), _ptr(which), wp, wb, _stream(stream)))
+
+
+def kf_page_compact(pages: Pages, keep, k: int, which=None, workspace=None, stream=None) -> None:
+    """keep: int32 [L,B,H,k], the tokens that each head keeps; which: int32 [B], or None: all."""
+    cs = pages.c_struct()
+    wp, wb = _ws(workspace)
+    _check(lib().kf_page_compact(C.byref(cs), _ptr(keep), k, _ptr(which), wp, wb, _stream(stream)))

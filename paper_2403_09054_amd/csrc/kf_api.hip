@@ -950,4 +950,241 @@ kf_status kf_beam_select(const kf_beams* b, const void* logits, const float* sco
     return KF_OK;
 }
 
+// What the kernels of a prompt attention take, but for its buffers; the bytes of its workspace.
+static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sums, size_t* bytes) {
+    if (!p) return fail(KF_EINVAL, "prompt description is NULL");
+    if (p->B < 1 || p->n < 1 || p->m < 1 || p->H < 1 || p->d < 1 || p->q_per_kv < 0)
+        return fail(KF_EINVAL, "sizes must be positive (B=%d n=%d m=%d H=%d d=%d q_per_kv=%d)", p->B, p->n, p->m, p->H, p->d, p->q_per_kv);
+    if (p->dtype != KF_F32 && p->dtype != KF_BF16 && p->dtype != KF_F16) return fail(KF_EINVAL, "unknown dtype %d", p->dtype);
+    if (!supported(p->dtype, p->d))
+        return fail(KF_EUNSUPPORTED, "dtype %d with head dimension %d is not built", p->dtype, p->d);
+    if (!isfinite(p->scale)) return fail(KF_EINVAL, "scale must be finite");
+    if (p->q_start && p->seq_n) return fail(KF_EINVAL, "rows are packed (q_start) or padded (seq_n), not both");
+    if (p->k_start && p->seq_m) return fail(KF_EINVAL, "keys are packed (k_start) or padded (seq_m), not both");
+    const int64_t G = p->q_per_kv > 1 ? p->q_per_kv : 1, HQ = p->H * G, d = p->d;
+    if (HQ > 1 << 24) return fail(KF_EINVAL, "too many heads");
+    if (p->n * G > 1 << 30 || p->m > 1 << 30) return fail(KF_EINVAL, "too many rows (n=%d, q_per_kv=%d, m=%d)", p->n, p->q_per_kv, p->m);
+    int64_t st[4][3];
+    const int64_t* given[4] = {p->q_stride, p->k_stride, p->v_stride, p->out_stride};
+    const int eb = p->dtype == KF_F32 ? 4 : 2;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t heads = i == 0 || i == 3 ? HQ : p->H, rows = i == 0 || i == 3 ? p->n : p->m;
+        const bool packed = i == 0 || i == 3 ? p->q_start != nullptr : p->k_start != nullptr;
+        for (int x = 0; x < 3; ++x) st[i][x] = given[i][x];
+        if (st[i][0] == 0 && st[i][1] == 0 && st[i][2] == 0) {
+            const bool by_token = packed || i == 3;
+            st[i][0] = heads * rows * d;
+            st[i][1] = by_token ? d : rows * d;
+            st[i][2] = by_token ? heads * d : d;
+        }
+        for (int x = 0; x < 3; ++x) {
+            if (st[i][x] < 0) return fail(KF_EINVAL, "strides must not be negative");
+            if ((st[i][x] * eb) % 16) return fail(KF_EINVAL, "strides must be multiples of 16 bytes");
+        }
+    }
+    a->q_sb = st[0][0], a->q_sh = st[0][1], a->q_st = st[0][2];
+    a->k_sb = st[1][0], a->k_sh = st[1][1], a->k_st = st[1][2];
+    a->v_sb = st[2][0], a->v_sh = st[2][1], a->v_st = st[2][2];
+    a->o_sb = st[3][0], a->o_sh = st[3][1], a->o_st = st[3][2];
+    a->q_start = p->q_start;
+    a->k_start = p->k_start;
+    a->seq_n = p->seq_n;
+    a->seq_m = p->seq_m;
+    a->slopes = p->alibi_slopes;
+    a->B = p->B;
+    a->n = p->n;
+    a->m = p->m;
+    a->H = p->H;
+    a->G = (int32_t)G;
+    a->sc = p->scale == 0.0f ? 1.0f : fminf(fabsf(p->scale) * kf::kLog2e, 3.4e38f);
+    a->q_keep = p->scale == 0.0f ? 0u : ~0u;
+    a->q_flip = p->scale < 0.0f ? (eb == 2 ? 0x80008000u : 0x80000000u) : 0u;
+    kf::plan_attend(a, p->d, p->dtype);
+    if (a->blocks > kMaxGrid - 8) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
+    *sums = align_up((size_t)a->ws_rows * a->S * p->d * 4, 256);
+    *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256);
+    return KF_OK;
+}
+
+size_t kf_prompt_workspace_bytes(const kf_prompt* p) {
+    kf::AttendArgs a;
+    size_t sums, bytes;
+    return check_prompt(p, &a, &sums, &bytes) == KF_OK ? bytes : 0;
+}
+
+kf_status kf_prompt_attend(const kf_prompt* p, const void* Q, const void* K, const void* V, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    kf::AttendArgs a;
+    size_t sums, bytes;
+    const kf_status st = check_prompt(p, &a, &sums, &bytes);
+    if (st != KF_OK) return st;
+    if (!Q || !K || !V || !out) return fail(KF_EINVAL, "Q, K, V and out must not be NULL");
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)out) & 15) return fail(KF_EINVAL, "Q, K, V and out must be 16-byte aligned");
+    const kf_status ws = check_ws(workspace, workspace_bytes, bytes);
+    if (ws != KF_OK) return ws;
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.out = out;
+    a.ws_o = (float*)((char*)workspace + 256);
+    a.ws_ml = (float2*)((char*)workspace + 256 + sums);
+    const hipError_t e = kf::launch_attend(a, p->d, p->dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(KF_EDEVICE, "prompt attention launch: %s", hipGetErrorString(e));
+    g_err[0] = 0;
+    return KF_OK;
+}
+
+// Workspace of the page calls: the error word, then, for one call at a time, the free pages that go out, what is copied and the
+// table before, or the records of a step's splits.
+static kf_status check_pages(const kf_pages* p, kf::PageArgs* a, size_t* bytes) {
+    if (!p) return fail(KF_EINVAL, "pages description is NULL");
+    if (p->L < 1 || p->B < 1 || p->H < 1 || p->d < 1 || p->pages < 1 || p->max_pages < 1)
+        return fail(KF_EINVAL, "sizes must be positive (L=%d B=%d H=%d d=%d pages=%d max_pages=%d)", p->L, p->B, p->H, p->d, p->pages, p->max_pages);
+    if (p->dtype != KF_BF16 && p->dtype != KF_F16) return fail(p->dtype == KF_F32 ? KF_EUNSUPPORTED : KF_EINVAL, "rows of dtype %d in 8-bit pages are not built", p->dtype);
+    if (p->d != 64 && p->d != 128 && p->d != 256) return fail(KF_EUNSUPPORTED, "head dimension %d is not built", p->d);
+    if (p->q_per_kv < 0) return fail(KF_EINVAL, "q_per_kv must not be negative");
+    if (!group_supported(p->q_per_kv)) return fail(KF_EUNSUPPORTED, "%d query heads per cached head is not built (1, 2, 4 or 8)", p->q_per_kv);
+    if (p->B > kf::kPageMaxRows) return fail(KF_EUNSUPPORTED, "%d sequences are not built (at most %d)", p->B, kf::kPageMaxRows);
+    const int64_t U = (int64_t)p->L * p->B * p->H;
+    if (U > (int64_t)1 << 24) return fail(KF_EINVAL, "too many units");
+    if (p->max_pages > 1 << 24 || (int64_t)p->B * p->max_pages > (int64_t)1 << 30) return fail(KF_EINVAL, "max_pages=%d is too large", p->max_pages);
+    memset(a, 0, sizeof(*a));
+    a->K = (uint8_t*)p->K;
+    a->V = (uint8_t*)p->V;
+    a->k_scale = p->k_scale;
+    a->v_scale = p->v_scale;
+    a->table = p->table;
+    a->len = p->len;
+    a->refs = p->refs;
+    a->L = p->L;
+    a->B = p->B;
+    a->H = p->H;
+    a->G = p->q_per_kv > 1 ? p->q_per_kv : 1;
+    a->pages = p->pages;
+    a->max_pages = p->max_pages;
+    const size_t tables = align_up((size_t)p->pages * 4, 256) + align_up((size_t)p->B * 8, 256) + align_up((size_t)p->B * p->max_pages * 4, 256);
+    const int32_t S = kf::page_most_splits(U, p->max_pages);
+    const size_t records = S > 1 ? align_up((size_t)U * S * a->G * p->d * 4, 256) + align_up((size_t)U * S * a->G * 8, 256) : 0;
+    *bytes = 256 + (tables > records ? tables : records);
+    return KF_OK;
+}
+
+// The checks of a call that launches, and the workspace's places.
+static kf_status begin_pages(const kf_pages* p, kf::PageArgs* a, void* workspace, size_t workspace_bytes) {
+    size_t bytes;
+    const kf_status st = check_pages(p, a, &bytes);
+    if (st != KF_OK) return st;
+    if (!p->K || !p->V || !p->k_scale || !p->v_scale || !p->table || !p->len || !p->refs) return fail(KF_EINVAL, "pages have a NULL buffer");
+    if (((uintptr_t)p->K | (uintptr_t)p->V) & 15) return fail(KF_EINVAL, "K and V must be 16-byte aligned");
+    const kf_status ws = check_ws(workspace, workspace_bytes, bytes);
+    if (ws != KF_OK) return ws;
+    char* w = (char*)workspace;
+    a->ws_err = (int32_t*)w + KF_WS_ERROR_WORD;
+    w += 256;
+    a->ws_list = (int32_t*)w;
+    w += align_up((size_t)p->pages * 4, 256);
+    a->ws_copy = (int2*)w;
+    w += align_up((size_t)p->B * 8, 256);
+    a->ws_old = (int32_t*)w;
+    return KF_OK;
+}
+static kf_status end_pages(hipError_t e, const char* what) {
+    if (e != hipSuccess) return fail(KF_EDEVICE, "%s launch: %s", what, hipGetErrorString(e));
+    g_err[0] = 0;
+    return KF_OK;
+}
+
+size_t kf_page_workspace_bytes(const kf_pages* p) {
+    kf::PageArgs a;
+    size_t bytes;
+    return check_pages(p, &a, &bytes) == KF_OK ? bytes : 0;
+}
+
+kf_status kf_page_reserve(const kf_pages* p, int32_t n, const int32_t* seq_n, void* workspace, size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    if (n < 1) return fail(KF_EINVAL, "n=%d must be positive", n);
+    a.n = n;
+    a.seq_n = seq_n;
+    return end_pages(kf::launch_page_reserve(a, (hipStream_t)stream), "page reservation");
+}
+
+kf_status kf_page_write(const kf_pages* p, const void* k, const void* v, int32_t n, int32_t rows, const int32_t* seq_n, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    if (!k || !v) return fail(KF_EINVAL, "k and v must not be NULL");
+    if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(KF_EINVAL, "k and v must be 16-byte aligned");
+    if (n < 1 || (rows != 0 && rows < n)) return fail(KF_EINVAL, "n=%d must be positive and not above rows=%d", n, rows);
+    if ((int64_t)p->L * p->B > 65535 || p->H > 65535)
+        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads exceed the largest launch", p->L, p->B, p->H);
+    a.k = k;
+    a.v = v;
+    a.n = n;
+    a.rows = rows ? rows : n;
+    a.seq_n = seq_n;
+    return end_pages(kf::launch_page_write(a, p->d, p->dtype, (hipStream_t)stream), "page write");
+}
+
+kf_status kf_page_step(const kf_pages* p, const void* q, const void* k_new, const void* v_new, float scale, const float* alibi_slopes,
+                       const int32_t* seq_n, int32_t m_hint, float* out, void* workspace, size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    if (!q || !k_new || !v_new || !out) return fail(KF_EINVAL, "q, k_new, v_new and out must not be NULL");
+    if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return fail(KF_EINVAL, "q, k_new and v_new must be 16-byte aligned");
+    if (!isfinite(scale)) return fail(KF_EINVAL, "scale must be finite");
+    const int64_t room = (int64_t)p->max_pages * KF_PAGE_TOKENS;
+    if (m_hint < 0 || m_hint > room) return fail(KF_EINVAL, "m_hint %d outside [0, %lld]", m_hint, (long long)room);
+    const int64_t U = (int64_t)p->L * p->B * p->H;
+    a.q = q;
+    a.k = k_new;
+    a.v = v_new;
+    a.out = out;
+    a.slopes = alibi_slopes;
+    a.seq_n = seq_n;
+    a.sc = scale * kf::kLog2e;
+    kf::plan_page_step(&a, U, m_hint ? m_hint : (int32_t)room);
+    if (U * a.S > kMaxGrid) return fail(KF_EUNSUPPORTED, "%lld units in %d splits each exceed the largest launch", (long long)U, a.S);
+    a.ws_o = (float*)((char*)workspace + 256);
+    a.ws_ml = (float2*)((char*)workspace + 256 + align_up((size_t)U * a.S * a.G * p->d * 4, 256));
+    return end_pages(kf::launch_page_step(a, U, p->d, p->dtype, (hipStream_t)stream), "page step");
+}
+
+kf_status kf_page_fork(const kf_pages* p, const int32_t* parent, void* workspace, size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    if (!parent) return fail(KF_EINVAL, "parent is NULL");
+    if (p->L > 65535) return fail(KF_EUNSUPPORTED, "%d layers exceed the largest launch", p->L);
+    a.which = parent;
+    return end_pages(kf::launch_page_fork(a, p->d, (hipStream_t)stream), "page fork");
+}
+
+kf_status kf_page_free(const kf_pages* p, const int32_t* which, void* workspace, size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    a.which = which;
+    return end_pages(kf::launch_page_free(a, (hipStream_t)stream), "page release");
+}
+
+kf_status kf_page_compact(const kf_pages* p, const int32_t* keep, int32_t k, const int32_t* which, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    kf::PageArgs a;
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    if (st != KF_OK) return st;
+    if (!keep) return fail(KF_EINVAL, "keep is NULL");
+    const int64_t room = (int64_t)p->max_pages * KF_PAGE_TOKENS;
+    if (k < 1 || k > room) return fail(KF_EINVAL, "k=%d outside [1, %lld]", k, (long long)room);
+    if ((int64_t)p->L * p->B > 65535 || p->H > 65535)
+        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads exceed the largest launch", p->L, p->B, p->H);
+    a.keep = keep;
+    a.kept = k;
+    a.which = which;
+    return end_pages(kf::launch_page_compact(a, p->d, (hipStream_t)stream), "page compaction");
+}
+
 }  // extern "C"

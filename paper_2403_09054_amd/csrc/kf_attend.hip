@@ -1,0 +1,389 @@
+// Attention over prompts for gfx950: causal, grouped heads, sequences of their own lengths.
+//
+//   x_ij = scale*<q_i, k_j> - slope*(p_i - j)    j <= p_i = i + nk - nq        (query i of nq, key j of nk)
+//   out_i = sum_j exp(x_ij - m_i) v_j / sum_j exp(x_ij - m_i)
+//
+// One pass over the keys with a running reference m and sum (in 32 bits); rows of both are never stored.  A wave takes 32 rows --
+// a row is a query of one of the G heads that share a cached head, head by head inside a position, so that a tile of keys serves
+// all of them -- and forms S^T = K Q^T and O^T = V^T P^T in tiles of 32 x 32: a lane then owns one row in both, its maximum and sum
+// need one exchange between the wave's halves, and the exponentials, rounded to the element type, are the second product's operand as
+// they lie.  (The order of the keys inside a product is free; the values' operand is read transposed from LDS in the same order.)
+// Tiles of K and V go from memory through registers into LDS, two buffers, swizzled so that both ways of reading meet each bank once.
+#include "kf_device.h"
+#include "kf_internal.h"
+#include "kf_prefill.h"
+
+namespace kf {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Keys of a tile: 32 KB of K and V together, or as much as two tiles leave for two workgroups on a compute unit.
+template <typename T, int D>
+constexpr int attend_keys() { return D * (int)sizeof(T) > 256 ? 32 : 64; }
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack_pair<bf16_t>(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
+template <>
+__device__ __forceinline__ uint32_t pack_pair<f16_t>(float a, float b) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b}); }
+
+// Whether a 16-byte piece holds an infinity or a NaN.
+template <typename T>
+__device__ __forceinline__ bool not_finite(const u32x4_t& v) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) bad |= (v[i] & 0x7F800000u) == 0x7F800000u;
+        else {
+            constexpr uint32_t e = __is_same(T, bf16_t) ? 0x7F80u : 0x7C00u;
+            bad |= (v[i] & e) == e || (v[i] & (e << 16)) == e << 16;
+        }
+    }
+    return bad;
+}
+template <typename T>
+__device__ __forceinline__ float element(const char* p) {
+    if constexpr (sizeof(T) == 4) return *(const float*)p;
+    else if constexpr (__is_same(T, bf16_t)) return __uint_as_float((uint32_t)*(const uint16_t*)p << 16);
+    else return (float)*(const _Float16*)p;
+}
+
+// Largest of a lane's and its partner's in the wave's other half.
+__device__ __forceinline__ float half_max(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// A reference is raised once a row's largest exponent is this far above it; terms stay below 2^8.
+constexpr float kAttendSlack = 8.0f;
+
+template <typename T, int D, int W, bool BIAS>
+__global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2)) attend_kernel(const AttendArgs a) {
+    constexpr int EB = sizeof(T), RB = D * EB, CH = RB / 16, NT = W * kWave, BK = attend_keys<T, D>(), NB = BK / 32;
+    constexpr int PT = BK * CH / NT;             // 16-byte pieces of a tile that a thread brings
+    constexpr int KS = RB / 32, DT = D / 32, ROWS = W * 32;
+    static_assert(BK * CH % NT == 0 && PT >= 1, "a tile is brought in whole rounds");
+    __shared__ __attribute__((aligned(16))) char kbuf[2][BK * RB];
+    __shared__ __attribute__((aligned(16))) char vbuf[2][BK * RB];
+    __shared__ int bad_s[2];                     // the tile whose values hold an infinity or a NaN
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 31, half = lane >> 5;
+
+    // an XCD takes a run of neighbouring workgroups: those of one cached head share its L2
+    const unsigned run = (gridDim.x + kXcds - 1) / kXcds, at = blockIdx.x % kXcds * run + blockIdx.x / kXcds;
+    if (at >= (unsigned)a.blocks) return;
+    const unsigned per = (unsigned)(a.tiles * a.S), unit = at / per, rest = at - unit * per;
+    const int qt = a.tiles - 1 - (int)(rest / (unsigned)a.S), split = (int)(rest % (unsigned)a.S);  // long walks first
+    const int h = (int)(unit / (unsigned)a.B), b = (int)(unit % (unsigned)a.B);
+
+    int64_t q0 = 0, k0 = 0;
+    int nq = a.n, nk = a.m;
+    if (a.q_start) q0 = a.q_start[b], nq = (int)min((int64_t)a.q_start[b + 1] - q0, (int64_t)0x7fffffff);
+    else if (a.seq_n) nq = a.seq_n[b];
+    if (a.k_start) k0 = a.k_start[b], nk = (int)min((int64_t)a.k_start[b + 1] - k0, (int64_t)0x7fffffff);
+    else if (a.seq_m) nk = a.seq_m[b];
+    if (nq < 1 || nq > a.n || nk < 0 || nk > a.m || q0 < 0 || k0 < 0) return;  // no such sequence
+    const int rows = nq * a.G, R0 = qt * ROWS;   // (n * G fits 31 bits: the host asks)
+    if (R0 >= rows) return;
+    const int off = nk - nq;
+    const char* Kh = (const char*)a.K + ((a.k_start ? k0 * a.k_st : b * a.k_sb) + h * a.k_sh) * EB;
+    const char* Vh = (const char*)a.V + ((a.k_start ? k0 * a.v_st : b * a.v_sb) + h * a.v_sh) * EB;
+    const int64_t krow = a.k_st * EB, vrow = a.v_st * EB;
+
+    // this lane's row
+    const int R = min(R0 + wv * 32 + n0, rows - 1), qi = R / a.G, qh = h * a.G + (R - qi * a.G), pos = off + qi;
+    const bool mine = R0 + wv * 32 + n0 < rows;
+    u32x4_t q[KS];
+    {
+        const char* p = (const char*)a.Q + ((a.q_start ? q0 * a.q_st : b * a.q_sb) + qh * a.q_sh + qi * a.q_st) * EB + half * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = (*(const u32x4_t*)(p + s * 32) & a.q_keep) ^ a.q_flip;
+    }
+    float slope = 0.0f;
+    if constexpr (BIAS) slope = a.slopes[qh] * kLog2e;
+
+    // tiles: the workgroup's rows see keys [0, kend)
+    const int kend = min(nk, off + min(R0 + ROWS - 1, rows - 1) / a.G + 1);
+    int t0 = 0, t1 = kend > 0 ? (kend + BK - 1) / BK : 0;
+    if (a.S > 1) {
+        const int each = (t1 + a.S - 1) / a.S;
+        t0 = min(split * each, t1);
+        t1 = min(t0 + each, t1);
+    }
+    const int first = off + min(R0 + wv * 32, rows - 1) / a.G, last = off + min(R0 + wv * 32 + 31, rows - 1) / a.G;  // of the wave
+    const int lowest = off + R0 / a.G;           // of the workgroup
+
+    u32x4_t kr[PT], vr[PT];
+    auto bring = [&](int t) {
+#pragma unroll
+        for (int x = 0; x < PT; ++x) {
+            const int p = tid + x * NT, row = min(t * BK + p / CH, nk - 1), c = p % CH;
+            kr[x] = *(const u32x4_t*)(Kh + row * krow + c * 16);
+            vr[x] = *(const u32x4_t*)(Vh + row * vrow + c * 16);
+        }
+    };
+    // Pieces of keys are read 16 rows a time at one place of the row, pieces of values 4 rows at 64 neighbouring bytes: in LDS a row's
+    // pieces are exchanged by the row's number, so that either way falls on all banks.
+    auto key_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 15) : c ^ (row >> 1 & 7); };
+    auto value_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; };
+    auto park = [&](int t, int buf) {
+        bool bad = false;
+#pragma unroll
+        for (int x = 0; x < PT; ++x) {
+            const int p = tid + x * NT, row = p / CH, c = p % CH;
+            *(u32x4_t*)(kbuf[buf] + row * RB + key_piece(row, c) * 16) = kr[x];
+            *(u32x4_t*)(vbuf[buf] + row * RB + value_piece(row, c) * 16) = vr[x];
+        }
+        if (t * BK + BK - 1 > lowest) {          // some row does not see all of the tile
+#pragma unroll
+            for (int x = 0; x < PT; ++x) bad |= not_finite<T>(vr[x]);
+            if (bad) bad_s[buf] = t;
+        }
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.0f);
+    float m = -INFINITY, l = 0.0f;
+
+    if (t0 < t1) {
+        if (tid < 2) bad_s[tid] = -1;
+        bring(t1 - 1);
+        __syncthreads();
+        park(t1 - 1, (t1 - 1) & 1);
+        __syncthreads();
+    }
+    for (int t = t1 - 1; t >= t0; --t) {         // from the diagonal
+        const int buf = t & 1;
+        if (t > t0) bring(t - 1);
+        if (t * BK <= last) {                    // else the wave's rows see nothing of it
+            const char* kt = kbuf[buf] + n0 * RB;
+            f32x16 s[NB];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                s[kb] = (f32x16)(0.0f);
+#pragma unroll
+                for (int g = 0; g < KS; ++g) {
+                    const uint4 k = *(const uint4*)(kt + kb * 32 * RB + key_piece(n0, 2 * g + half) * 16);
+                    s[kb] = Mma<T>::group(k, __builtin_bit_cast(uint4, q[g]), s[kb]);
+                }
+            }
+            const int key0 = t * BK + half * 4;
+            float sc = a.sc;
+            if constexpr (BIAS) {
+                const float base = slope * (float)(key0 - pos);
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kb][r] = fmaf(s[kb][r], a.sc, fmaf(slope, (float)(kb * 32 + (r >> 2) * 8 + (r & 3)), base));
+                sc = 1.0f;
+            }
+            if (t * BK + BK - 1 > first) {
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kb][r] = key0 + kb * 32 + (r >> 2) * 8 + (r & 3) > pos ? -INFINITY : s[kb][r];
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+            top = half_max(top) * sc;
+            if (__any(top > m + kAttendSlack || m == -INFINITY)) {
+                const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : hw_exp2(m - to);
+                m = to;
+                l *= by;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[i] *= by;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] = hw_exp2(BIAS ? s[kb][r] - ref : fmaf(s[kb][r], sc, -ref));
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) l += s[kb][r];
+            const char* vt = vbuf[buf];
+            if (bad_s[buf] == t) {
+                // a value that some rows must not see is no number, and 0 times it would be none either: key by key, by the rows that see it
+#pragma unroll 1
+                for (int r = 0; r < 16; ++r) {
+#pragma unroll
+                    for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+                        for (int hh = 0; hh < 2; ++hh) {
+                            const int key = kb * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
+                            const float p = __shfl(s[kb][0], n0 + hh * 32, kWave);
+                            if (t * BK + key <= pos) {
+#pragma unroll
+                                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                                    for (int y = 0; y < 16; ++y) {
+                                        const int byte = (i * 32 + acc_row(y, half)) * EB;
+                                        o[i][y] = fmaf(p, element<T>(vt + key * RB + value_piece(key, byte / 16) * 16 + byte % 16), o[i][y]);
+                                    }
+                            }
+                        }
+                        const float p0 = s[kb][0];
+#pragma unroll
+                        for (int y = 0; y < 15; ++y) s[kb][y] = s[kb][y + 1];
+                        s[kb][15] = p0;
+                    }
+                }
+            } else if constexpr (EB == 2) {
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint4 p;
+                        p.x = pack_pair<T>(s[kb][8 * x], s[kb][8 * x + 1]);
+                        p.y = pack_pair<T>(s[kb][8 * x + 2], s[kb][8 * x + 3]);
+                        p.z = pack_pair<T>(s[kb][8 * x + 4], s[kb][8 * x + 5]);
+                        p.w = pack_pair<T>(s[kb][8 * x + 6], s[kb][8 * x + 7]);
+                        // of 16 lanes each four bring 16 neighbouring elements of a row, and a lane receives its element of the four rows
+                        const int row = kb * 32 + x * 16 + half * 4 + (lane >> 2 & 3), c = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+#pragma unroll
+                        for (int i = 0; i < DT; ++i) {
+                            const char* p0 = vt + row * RB + value_piece(row, i * 4 + c) * 16 + (lane & 1) * 8;
+                            const char* p1 = vt + (row + 8) * RB + value_piece(row + 8, i * 4 + c) * 16 + (lane & 1) * 8;
+                            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p0));
+                            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p1));
+                            const uint2 u = __builtin_bit_cast(uint2, lo), v = __builtin_bit_cast(uint2, hi);
+                            o[i] = Mma<T>::group(make_uint4(u.x, u.y, v.x, v.y), p, o[i]);
+                        }
+                    }
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+#pragma unroll
+                        for (int i = 0; i < DT; ++i) {
+                            const int byte = (i * 32 + n0) * 4;
+                            const float v = *(const float*)(vt + row * RB + value_piece(row, byte / 16) * 16 + byte % 16);
+                            o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[kb][r], o[i], 0, 0, 0);
+                        }
+                    }
+            }
+        }
+        if (t > t0) park(t - 1, buf ^ 1);
+        __syncthreads();
+    }
+    l = half_sum(l);
+    if (!mine) return;
+    if (a.S > 1) {
+        const int64_t row = ((int64_t)unit * a.tiles * ROWS + R) * a.S + split;
+        if (half == 0) a.ws_ml[row] = make_float2(m, l);
+        float* w = a.ws_o + row * D;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                *(float4*)(w + i * 32 + y * 8 + half * 4) = make_float4(o[i][4 * y], o[i][4 * y + 1], o[i][4 * y + 2], o[i][4 * y + 3]);
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    char* w = (char*)a.out + ((a.q_start ? q0 * a.o_st : b * a.o_sb) + qh * a.o_sh + qi * a.o_st) * EB;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const float v0 = o[i][4 * y] * inv, v1 = o[i][4 * y + 1] * inv, v2 = o[i][4 * y + 2] * inv, v3 = o[i][4 * y + 3] * inv;
+            char* p = w + (i * 32 + y * 8 + half * 4) * EB;
+            if constexpr (EB == 4) *(float4*)p = make_float4(v0, v1, v2, v3);
+            else *(uint2*)p = make_uint2(pack_pair<T>(v0, v1), pack_pair<T>(v2, v3));
+        }
+}
+
+// Joins the parts of a row: one wave a row, a lane takes D / 64 elements.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int rows_pad) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), unit = at / rows_pad;
+    const int R = (int)(at - unit * rows_pad), h = (int)(unit / a.B), b = (int)(unit % a.B);
+    if (h >= a.H) return;
+    int64_t q0 = 0, k0 = 0;
+    int nq = a.n, nk = a.m;
+    if (a.q_start) q0 = a.q_start[b], nq = (int)min((int64_t)a.q_start[b + 1] - q0, (int64_t)0x7fffffff);
+    else if (a.seq_n) nq = a.seq_n[b];
+    if (a.k_start) k0 = a.k_start[b], nk = (int)min((int64_t)a.k_start[b + 1] - k0, (int64_t)0x7fffffff);
+    else if (a.seq_m) nk = a.seq_m[b];
+    if (nq < 1 || nq > a.n || nk < 0 || nk > a.m || q0 < 0 || k0 < 0 || R >= nq * a.G) return;
+    const int qi = R / a.G, qh = h * a.G + (R - qi * a.G);
+    const int64_t row = at * a.S;
+    float m = -INFINITY;
+    for (int s = 0; s < a.S; ++s) m = fmaxf(m, a.ws_ml[row + s].x);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.0f;
+    for (int s = 0; s < a.S; ++s) {
+        const float2 ml = a.ws_ml[row + s];
+        const float by = hw_exp2(ml.x - ref);
+        l = fmaf(by, ml.y, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(by, a.ws_o[(row + s) * D + lane * E + e], x[e]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T* w = (T*)a.out + (a.q_start ? q0 * a.o_st : b * a.o_sb) + qh * a.o_sh + qi * a.o_st + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if constexpr (sizeof(T) == 4) w[e] = x[e] * inv;
+        else w[e].bits = (uint16_t)pack_pair<T>(x[e] * inv, 0.0f);
+    }
+}
+
+constexpr int kAttendWaves = 4;
+
+void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
+    a->tiles = (int32_t)(((int64_t)a->n * a->G + kAttendWaves * 32 - 1) / (kAttendWaves * 32));
+    a->S = 1;
+    const int64_t blocks = (int64_t)a->B * a->H * a->tiles;
+    const int32_t keys = d * (dtype == KF_F32 ? 4 : 2) > 256 ? 32 : 64, walk = (a->m + keys - 1) / keys;
+    if (blocks < 256) {
+        int64_t S = 512 / blocks;
+        if (S > walk / 4) S = walk / 4;
+        if (S > 64) S = 64;
+        if (S > 1) a->S = (int32_t)S;
+    }
+    a->blocks = blocks * a->S;
+    a->ws_rows = a->S > 1 ? (int64_t)a->B * a->H * a->tiles * kAttendWaves * 32 : 0;
+}
+
+template <typename T, int D>
+static hipError_t launch_attend_d(const AttendArgs& a, hipStream_t st) {
+    const int64_t run = (a.blocks + kXcds - 1) / kXcds;
+    const dim3 grid((unsigned)(run * kXcds)), block(kAttendWaves * kWave);
+    if (a.slopes) hipLaunchKernelGGL((attend_kernel<T, D, kAttendWaves, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attend_kernel<T, D, kAttendWaves, false>), grid, block, 0, st, a);
+    if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * kAttendWaves * 32);
+    return hipGetLastError();
+}
+
+hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream) {
+    if (dtype == KF_BF16) {
+        if (d == 64) return launch_attend_d<bf16_t, 64>(a, stream);
+        if (d == 128) return launch_attend_d<bf16_t, 128>(a, stream);
+        if (d == 256) return launch_attend_d<bf16_t, 256>(a, stream);
+    } else if (dtype == KF_F16) {
+        if (d == 64) return launch_attend_d<f16_t, 64>(a, stream);
+        if (d == 128) return launch_attend_d<f16_t, 128>(a, stream);
+        if (d == 256) return launch_attend_d<f16_t, 256>(a, stream);
+    } else if (dtype == KF_F32) {
+        if (d == 64) return launch_attend_d<float, 64>(a, stream);
+        if (d == 128) return launch_attend_d<float, 128>(a, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace kf

@@ -307,4 +307,65 @@ struct BeamPlan {
 BeamPlan plan_beam(int64_t rows, int32_t W, int32_t V, int32_t dtype);
 hipError_t launch_beam(const BeamArgs& a, int32_t R, int32_t dtype, const BeamPlan& p, hipStream_t stream);
 
+// ------------------------------------------------------------------ attention over prompts (kf_attend.hip)
+struct AttendArgs {
+    const void* Q;
+    const void* K;
+    const void* V;
+    void* out;
+    const int32_t* q_start;  // [B + 1] first row of a packed sequence, or NULL
+    const int32_t* k_start;
+    const int32_t* seq_n;    // [B] rows of a sequence, or NULL: n
+    const int32_t* seq_m;
+    const float* slopes;
+    int64_t q_sb, q_sh, q_st, k_sb, k_sh, k_st, v_sb, v_sh, v_st, o_sb, o_sh, o_st;  // elements between sequences, heads, tokens
+    int32_t B, n, m, H, G;
+    float sc;                // |scale| * log2(e); the queries take the scale's sign, or zero with it
+    uint32_t q_keep, q_flip;
+    int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys
+    int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
+    float* ws_o;             // [ws_rows][S][d]
+    float2* ws_ml;           // [ws_rows][S] reference and sum
+};
+void plan_attend(AttendArgs* a, int32_t d, int32_t dtype);
+hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream);
+
+// ------------------------------------------------------------------ pages of an 8-bit cache (kf_pages.hip)
+constexpr int32_t kPageMaxRows = 8192;  // sequences: the table's launches hold a word of each in LDS
+struct PageArgs {
+    uint8_t* K;              // [L][pages][H][64][d]
+    uint8_t* V;              // [L][pages][H][d][64]
+    float* k_scale;          // [L][pages][H]
+    float* v_scale;
+    int32_t* table;          // [B][max_pages]
+    int32_t* len;            // [B]
+    int32_t* refs;           // [pages]
+    const void* q;
+    const void* k;           // new rows: [L][B][H][rows][d]
+    const void* v;
+    float* out;
+    const float* slopes;
+    const int32_t* seq_n;    // [B] new tokens of a sequence, or NULL: n
+    const int32_t* which;    // [B] rows that a call is about, or NULL: all; of a fork: the parents
+    const int32_t* keep;     // [L][B][H][k]
+    int32_t* ws_err;         // [1]
+    int32_t* ws_list;        // [pages] free pages that go out
+    int2* ws_copy;           // [B] page to copy and its place; of a compaction: the length before, or 0
+    int32_t* ws_old;         // [B][max_pages] the table before
+    float* ws_o;             // [U][S][G][d] splits' sums
+    float2* ws_ml;           // [U][S][G] their references and sums of exponentials
+    int32_t L, B, H, G, pages, max_pages;
+    int32_t n, rows, kept;   // new tokens at most, rows a head of k and v has room for, tokens that stay
+    int32_t S, chunk;        // splits of a unit, pages of a split
+    float sc;                // scale * log2(e)
+};
+int32_t page_most_splits(int64_t U, int32_t max_pages);
+void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint);
+hipError_t launch_page_step(const PageArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
+hipError_t launch_page_write(const PageArgs& a, int32_t d, int32_t dtype, hipStream_t stream);
+hipError_t launch_page_reserve(const PageArgs& a, hipStream_t stream);
+hipError_t launch_page_free(const PageArgs& a, hipStream_t stream);
+hipError_t launch_page_fork(const PageArgs& a, int32_t d, hipStream_t stream);
+hipError_t launch_page_compact(const PageArgs& a, int32_t d, hipStream_t stream);
+
 }  // namespace kf
