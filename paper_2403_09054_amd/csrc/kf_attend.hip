@@ -29,25 +29,24 @@ __device__ __forceinline__ uint32_t pack_pair<bf16_t>(float a, float b) { return
 template <>
 __device__ __forceinline__ uint32_t pack_pair<f16_t>(float a, float b) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b}); }
 
-// Whether a 16-byte piece holds an infinity or a NaN.
+// A 16-byte piece with zeros in the place of infinities and NaNs; whether there were any.
 template <typename T>
-__device__ __forceinline__ bool not_finite(const u32x4_t& v) {
+__device__ __forceinline__ bool clean_piece(u32x4_t& v) {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) bad |= (v[i] & 0x7F800000u) == 0x7F800000u;
-        else {
+        if constexpr (sizeof(T) == 4) {
+            const bool odd = (v[i] & 0x7F800000u) == 0x7F800000u;
+            v[i] = odd ? 0u : v[i];
+            bad |= odd;
+        } else {
             constexpr uint32_t e = __is_same(T, bf16_t) ? 0x7F80u : 0x7C00u;
-            bad |= (v[i] & e) == e || (v[i] & (e << 16)) == e << 16;
+            const bool lo = (v[i] & e) == e, hi = (v[i] & (e << 16)) == e << 16;
+            v[i] = (lo ? 0u : v[i] & 0xFFFFu) | (hi ? 0u : v[i] & 0xFFFF0000u);
+            bad |= lo || hi;
         }
     }
     return bad;
-}
-template <typename T>
-__device__ __forceinline__ float element(const char* p) {
-    if constexpr (sizeof(T) == 4) return *(const float*)p;
-    else if constexpr (__is_same(T, bf16_t)) return __uint_as_float((uint32_t)*(const uint16_t*)p << 16);
-    else return (float)*(const _Float16*)p;
 }
 
 // Largest of a lane's and its partner's in the wave's other half.
@@ -71,7 +70,7 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
     static_assert(BK * CH % NT == 0 && PT >= 1, "a tile is brought in whole rounds");
     __shared__ __attribute__((aligned(16))) char kbuf[2][BK * RB];
     __shared__ __attribute__((aligned(16))) char vbuf[2][BK * RB];
-    __shared__ int bad_s[2];                     // the tile whose values hold an infinity or a NaN
+    __shared__ int bad_s;                        // a tile of which some rows do not see all holds a value that is infinite or no number
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 31, half = lane >> 5;
 
     // an XCD takes a run of neighbouring workgroups: those of one cached head share its L2
@@ -132,17 +131,16 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
     auto key_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 15) : c ^ (row >> 1 & 7); };
     auto value_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; };
     auto park = [&](int t, int buf) {
-        bool bad = false;
+        if (t * BK + BK - 1 > lowest) {          // some row does not see all of the tile: see the end
+#pragma unroll
+            for (int x = 0; x < PT; ++x)
+                if (clean_piece<T>(vr[x])) bad_s = 1;
+        }
 #pragma unroll
         for (int x = 0; x < PT; ++x) {
             const int p = tid + x * NT, row = p / CH, c = p % CH;
             *(u32x4_t*)(kbuf[buf] + row * RB + key_piece(row, c) * 16) = kr[x];
             *(u32x4_t*)(vbuf[buf] + row * RB + value_piece(row, c) * 16) = vr[x];
-        }
-        if (t * BK + BK - 1 > lowest) {          // some row does not see all of the tile
-#pragma unroll
-            for (int x = 0; x < PT; ++x) bad |= not_finite<T>(vr[x]);
-            if (bad) bad_s[buf] = t;
         }
     };
 
@@ -152,7 +150,7 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
     float m = -INFINITY, l = 0.0f;
 
     if (t0 < t1) {
-        if (tid < 2) bad_s[tid] = -1;
+        if (tid == 0) bad_s = 0;
         bring(t1 - 1);
         __syncthreads();
         park(t1 - 1, (t1 - 1) & 1);
@@ -212,74 +210,63 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
 #pragma unroll
                 for (int r = 0; r < 16; ++r) l += s[kb][r];
             const char* vt = vbuf[buf];
-            if (bad_s[buf] == t) {
-                // a value that some rows must not see is no number, and 0 times it would be none either: key by key, by the rows that see it
-#pragma unroll 1
-                for (int r = 0; r < 16; ++r) {
+            // Operand x of the values, rows i * 32 .. of it: of 16 lanes each four bring 16 neighbouring elements of a key, and a lane
+            // receives its element of the four keys.  In fp32 four products take one key of either half each.
+            auto values = [&](int x, int i) {
+                if constexpr (EB == 2) {
+                    const int row = x * 16 + half * 4 + (lane >> 2 & 3), c = i * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + row * RB + value_piece(row, c) * 16 + (lane & 1) * 8));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (row + 8) * RB + value_piece(row + 8, c) * 16 + (lane & 1) * 8));
+                    const uint2 u = __builtin_bit_cast(uint2, lo), v = __builtin_bit_cast(uint2, hi);
+                    return make_uint4(u.x, u.y, v.x, v.y);
+                } else {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int kb = 0; kb < NB; ++kb) {
-#pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            const int key = kb * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
-                            const float p = __shfl(s[kb][0], n0 + hh * 32, kWave);
-                            if (t * BK + key <= pos) {
-#pragma unroll
-                                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                                    for (int y = 0; y < 16; ++y) {
-                                        const int byte = (i * 32 + acc_row(y, half)) * EB;
-                                        o[i][y] = fmaf(p, element<T>(vt + key * RB + value_piece(key, byte / 16) * 16 + byte % 16), o[i][y]);
-                                    }
-                            }
-                        }
-                        const float p0 = s[kb][0];
-#pragma unroll
-                        for (int y = 0; y < 15; ++y) s[kb][y] = s[kb][y + 1];
-                        s[kb][15] = p0;
+                    for (int y = 0; y < 4; ++y) {
+                        const int row = x * 8 + half * 4 + y, byte = (i * 32 + n0) * 4;
+                        w[y] = *(const uint32_t*)(vt + row * RB + value_piece(row, byte / 16) * 16 + byte % 16);
                     }
+                    return make_uint4(w[0], w[1], w[2], w[3]);
                 }
-            } else if constexpr (EB == 2) {
+            };
+            constexpr int XS = EB == 2 ? 2 : 4, PX = 16 / XS;  // operands of 32 keys, terms of each
 #pragma unroll
-                for (int kb = 0; kb < NB; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        uint4 p;
-                        p.x = pack_pair<T>(s[kb][8 * x], s[kb][8 * x + 1]);
-                        p.y = pack_pair<T>(s[kb][8 * x + 2], s[kb][8 * x + 3]);
-                        p.z = pack_pair<T>(s[kb][8 * x + 4], s[kb][8 * x + 5]);
-                        p.w = pack_pair<T>(s[kb][8 * x + 6], s[kb][8 * x + 7]);
-                        // of 16 lanes each four bring 16 neighbouring elements of a row, and a lane receives its element of the four rows
-                        const int row = kb * 32 + x * 16 + half * 4 + (lane >> 2 & 3), c = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+                for (int x = 0; x < XS; ++x) {
+                    uint32_t w[4];
 #pragma unroll
-                        for (int i = 0; i < DT; ++i) {
-                            const char* p0 = vt + row * RB + value_piece(row, i * 4 + c) * 16 + (lane & 1) * 8;
-                            const char* p1 = vt + (row + 8) * RB + value_piece(row + 8, i * 4 + c) * 16 + (lane & 1) * 8;
-                            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p0));
-                            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p1));
-                            const uint2 u = __builtin_bit_cast(uint2, lo), v = __builtin_bit_cast(uint2, hi);
-                            o[i] = Mma<T>::group(make_uint4(u.x, u.y, v.x, v.y), p, o[i]);
-                        }
+                    for (int y = 0; y < 4; ++y) {
+                        if constexpr (EB == 2) w[y] = pack_pair<T>(s[kb][x * PX + 2 * y], s[kb][x * PX + 2 * y + 1]);
+                        else w[y] = __float_as_uint(s[kb][x * PX + y]);
                     }
-            } else {
 #pragma unroll
-                for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int row = kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-#pragma unroll
-                        for (int i = 0; i < DT; ++i) {
-                            const int byte = (i * 32 + n0) * 4;
-                            const float v = *(const float*)(vt + row * RB + value_piece(row, byte / 16) * 16 + byte % 16);
-                            o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[kb][r], o[i], 0, 0, 0);
-                        }
-                    }
-            }
+                    for (int i = 0; i < DT; ++i) o[i] = Mma<T>::group(values(kb * XS + x, i), make_uint4(w[0], w[1], w[2], w[3]), o[i]);
+                }
         }
         if (t > t0) park(t - 1, buf ^ 1);
         __syncthreads();
     }
     l = half_sum(l);
     if (!mine) return;
+    if (t0 < t1 && bad_s) {
+        // 0 times an infinity would reach the rows that do not see it: such values were left out of the products with tiles of which
+        // some rows do not see all, and go to the rows that do here
+#pragma unroll 1
+        for (int j = max(t0, (lowest + 1) / BK) * BK; j <= min(pos, t1 * BK - 1); ++j) {
+            const char* row = Vh + j * vrow + half * 4 * EB;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int y = 0; y < 16; ++y) {
+                    const char* p = row + (i * 32 + acc_row(y, 0)) * EB;
+                    float v;
+                    if constexpr (EB == 4) v = *(const float*)p;
+                    else v = __is_same(T, bf16_t) ? __uint_as_float((uint32_t)*(const uint16_t*)p << 16) : (float)*(const _Float16*)p;
+                    o[i][y] += (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? v : 0.0f;
+                }
+        }
+    }
     if (a.S > 1) {
         const int64_t row = ((int64_t)unit * a.tiles * ROWS + R) * a.S + split;
         if (half == 0) a.ws_ml[row] = make_float2(m, l);
