@@ -432,7 +432,7 @@ kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *sco
  * Logits, softmax and sums have 32 bits; with 16-bit elements the probabilities are rounded to the element type for their
  * product with V.  A row of out is rounded once.
  *   strides : elements between sequences, heads, tokens; all three zero: Q [B][H*q_per_kv][n][d], K and V [B][H][m][d] (a layer of a
- *             cache with cap = m), out [B][n][H*q_per_kv][d]; of packed rows: [tokens][heads][d]
+ *             cache with cap = m), out [B][n][H*q_per_kv][d]; of packed rows: [tokens][heads][d].  Tokens of K and V lie at most 2^27 bytes apart.
  *   q_start, k_start : DEVICE [B+1] or NULL.  Packed sequences: b's rows are tokens start[b] .. start[b+1]-1 of one list (the
  *             stride between sequences is not used); q_start is that of Q and out, k_start of K and V
  *   seq_n, seq_m : DEVICE [B] or NULL.  Padded sequences: b has seq_n[b] of n rows, seq_m[b] of m keys.  Not together with

@@ -961,6 +961,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     if (!isfinite(p->scale)) return fail(KF_EINVAL, "scale must be finite");
     if (p->q_start && p->seq_n) return fail(KF_EINVAL, "rows are packed (q_start) or padded (seq_n), not both");
     if (p->k_start && p->seq_m) return fail(KF_EINVAL, "keys are packed (k_start) or padded (seq_m), not both");
+    if (p->alibi_slopes && p->scale != 0.0f && fabsf(p->scale) < 0x1p-60f) return fail(KF_EUNSUPPORTED, "a position bias beside a scale below 2^-60 is not built");
     const int64_t G = p->q_per_kv > 1 ? p->q_per_kv : 1, HQ = p->H * G, d = p->d;
     if (HQ > 1 << 24) return fail(KF_EINVAL, "too many heads");
     if (p->n * G > 1 << 30 || p->m > 1 << 30) return fail(KF_EINVAL, "too many rows (n=%d, q_per_kv=%d, m=%d)", p->n, p->q_per_kv, p->m);
@@ -982,6 +983,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
             if ((st[i][x] * eb) % 16) return fail(KF_EINVAL, "strides must be multiples of 16 bytes");
         }
     }
+    if (st[1][2] * eb > (int64_t)1 << 27 || st[2][2] * eb > (int64_t)1 << 27) return fail(KF_EUNSUPPORTED, "tokens of K and V more than 2^27 bytes apart are not built");
     a->q_sb = st[0][0], a->q_sh = st[0][1], a->q_st = st[0][2];
     a->k_sb = st[1][0], a->k_sh = st[1][1], a->k_st = st[1][2];
     a->v_sb = st[2][0], a->v_sh = st[2][1], a->v_st = st[2][2];

@@ -17,10 +17,23 @@ namespace kf {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) char lds_char;
 
-// Keys of a tile: 32 KB of K and V together, or as much as two tiles leave for two workgroups on a compute unit.
-template <typename T, int D>
-constexpr int attend_keys() { return D * (int)sizeof(T) > 256 ? 32 : 64; }
+// 16 bytes a lane from memory to LDS, at `lds` (the wave's) + 16 * lane.  The compiler does not know of them: whoever reads them waits for
+// vmcnt(0) and the workgroup first.  (Its own form of this waits for all of them ahead of any read of LDS.)
+__device__ __forceinline__ void to_lds(uint32_t lds, const char* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void to_lds(uint32_t lds, const char* p) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+
+// What a workgroup does: WR waves of 32 rows, times WK waves that share each tile's keys; SB blocks of 32 keys are a step of a wave, NB are
+// a tile.
+template <int WR_, int WK_, int SB_, int NB_>
+struct AttendShape {
+    static constexpr int WR = WR_, WK = WK_, SB = SB_, NB = NB_;
+};
 
 template <typename T>
 __device__ __forceinline__ uint32_t pack_pair(float a, float b);
@@ -62,16 +75,21 @@ __device__ __forceinline__ float half_sum(float v) {
 // A reference is raised once a row's largest exponent is this far above it; terms stay below 2^8.
 constexpr float kAttendSlack = 8.0f;
 
-template <typename T, int D, int W, bool BIAS>
-__global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2)) attend_kernel(const AttendArgs a) {
-    constexpr int EB = sizeof(T), RB = D * EB, CH = RB / 16, NT = W * kWave, BK = attend_keys<T, D>(), NB = BK / 32;
+template <typename T, int D, typename SHAPE, bool BIAS>
+__global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeof(T) > 256 || D * (int)sizeof(T) * SHAPE::NB > 640 ? 1 : 2)) attend_kernel(const AttendArgs a) {
+    constexpr int WR = SHAPE::WR, WK = SHAPE::WK, SB = SHAPE::SB, NB = SHAPE::NB, W = WR * WK, US = NB / (WK * SB);
+    constexpr int EB = sizeof(T), RB = D * EB, CH = RB / 16, NT = W * kWave, BK = NB * 32, AHEAD = WK * SB * 32;
     constexpr int PT = BK * CH / NT;             // 16-byte pieces of a tile that a thread brings
-    constexpr int KS = RB / 32, DT = D / 32, ROWS = W * 32;
-    static_assert(BK * CH % NT == 0 && PT >= 1, "a tile is brought in whole rounds");
-    __shared__ __attribute__((aligned(16))) char kbuf[2][BK * RB];
-    __shared__ __attribute__((aligned(16))) char vbuf[2][BK * RB];
+    constexpr int KS = RB / 32, DT = D / 32, ROWS = WR * 32;
+    static_assert(BK * CH % NT == 0 && PT >= 1 && US * WK * SB == NB, "a tile is brought in whole rounds and used in whole steps");
+    constexpr int JOIN = (WK - 1) * WR * (D * 32 * 4 + 512);  // what the waves that share rows leave at the end
+    constexpr int LDS = 4 * BK * RB > JOIN ? 4 * BK * RB : JOIN;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    char(*const kbuf)[BK * RB] = (char(*)[BK * RB]) lds;
+    char(*const vbuf)[BK * RB] = kbuf + 2;
     __shared__ int bad_s;                        // a tile of which some rows do not see all holds a value that is infinite or no number
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 31, half = lane >> 5;
+    const int wr = wv % WR, wk = wv / WR;
 
     // an XCD takes a run of neighbouring workgroups: those of one cached head share its L2
     const unsigned run = (gridDim.x + kXcds - 1) / kXcds, at = blockIdx.x % kXcds * run + blockIdx.x / kXcds;
@@ -95,8 +113,8 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
     const int64_t krow = a.k_st * EB, vrow = a.v_st * EB;
 
     // this lane's row
-    const int R = min(R0 + wv * 32 + n0, rows - 1), qi = R / a.G, qh = h * a.G + (R - qi * a.G), pos = off + qi;
-    const bool mine = R0 + wv * 32 + n0 < rows;
+    const int R = min(R0 + wr * 32 + n0, rows - 1), qi = R / a.G, qh = h * a.G + (R - qi * a.G), pos = off + qi;
+    const bool mine = R0 + wr * 32 + n0 < rows;
     u32x4_t q[KS];
     {
         const char* p = (const char*)a.Q + ((a.q_start ? q0 * a.q_st : b * a.q_sb) + qh * a.q_sh + qi * a.q_st) * EB + half * 16;
@@ -104,7 +122,7 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
         for (int s = 0; s < KS; ++s) q[s] = (*(const u32x4_t*)(p + s * 32) & a.q_keep) ^ a.q_flip;
     }
     float slope = 0.0f;
-    if constexpr (BIAS) slope = a.slopes[qh] * kLog2e;
+    if constexpr (BIAS) slope = a.slopes[qh] * kLog2e / a.sc;
 
     // tiles: the workgroup's rows see keys [0, kend)
     const int kend = min(nk, off + min(R0 + ROWS - 1, rows - 1) / a.G + 1);
@@ -114,142 +132,230 @@ __global__ void __launch_bounds__(W * kWave, (D * (int)sizeof(T) > 256 ? 1 : 2))
         t0 = min(split * each, t1);
         t1 = min(t0 + each, t1);
     }
-    const int first = off + min(R0 + wv * 32, rows - 1) / a.G, last = off + min(R0 + wv * 32 + 31, rows - 1) / a.G;  // of the wave
+    const int first = off + min(R0 + wr * 32, rows - 1) / a.G;  // of the wave
+    const int last = R0 + wr * 32 < rows ? off + min(R0 + wr * 32 + 31, rows - 1) / a.G : -1;
     const int lowest = off + R0 / a.G;           // of the workgroup
 
-    u32x4_t kr[PT], vr[PT];
-    auto bring = [&](int t) {
-#pragma unroll
-        for (int x = 0; x < PT; ++x) {
-            const int p = tid + x * NT, row = min(t * BK + p / CH, nk - 1), c = p % CH;
-            kr[x] = *(const u32x4_t*)(Kh + row * krow + c * 16);
-            vr[x] = *(const u32x4_t*)(Vh + row * vrow + c * 16);
-        }
-    };
     // Pieces of keys are read 16 rows a time at one place of the row, pieces of values 4 rows at 64 neighbouring bytes: in LDS a row's
     // pieces are exchanged by the row's number, so that either way falls on all banks.
     auto key_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 15) : c ^ (row >> 1 & 7); };
     auto value_piece = [](int row, int c) { return CH >= 16 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; };
-    auto park = [&](int t, int buf) {
-        if (t * BK + BK - 1 > lowest) {          // some row does not see all of the tile: see the end
+    // Tiles go from memory straight to LDS: an instruction of a wave fills 1 KB, a lane 16 bytes of it, so what a lane asks for is the
+    // piece that belongs where it writes.  A wave's instructions lie RPX rows apart: the rows' part of an address that the wave shares
+    // is the scalar unit's.  (The host refuses rows so far apart that the rest needs more than 32 bits.)
+    constexpr int RPX = NT / CH, NV = RPX % 16 == 0 ? 1 : 16 / RPX;
+    uint32_t koff[NV], voff[NV];
 #pragma unroll
-            for (int x = 0; x < PT; ++x)
-                if (clean_piece<T>(vr[x])) bad_s = 1;
-        }
+    for (int x = 0; x < NV; ++x) {
+        const int row = tid / CH, c = tid % CH;
+        koff[x] = (uint32_t)row * (uint32_t)krow + key_piece(row + x * RPX, c) * 16;
+        voff[x] = (uint32_t)row * (uint32_t)vrow + value_piece(row + x * RPX, c) * 16;
+    }
+    const uint32_t klds = (uint32_t)(uintptr_t)(lds_char*)kbuf + wv * 1024, vlds = (uint32_t)(uintptr_t)(lds_char*)vbuf + wv * 1024;
+    // rows [r0, r0 + BK) of K or V; what lies outside the sequence is its nearest row again
+    auto bring_rows = [&](int r0, const char* base, int64_t pitch, uint32_t lds, const uint32_t (&off)[NV], auto piece) {
+        if (r0 >= 0 && r0 + BK <= nk) {
+            const char* p = base + (int64_t)r0 * pitch;
 #pragma unroll
-        for (int x = 0; x < PT; ++x) {
-            const int p = tid + x * NT, row = p / CH, c = p % CH;
-            *(u32x4_t*)(kbuf[buf] + row * RB + key_piece(row, c) * 16) = kr[x];
-            *(u32x4_t*)(vbuf[buf] + row * RB + value_piece(row, c) * 16) = vr[x];
+            for (int x = 0; x < PT; ++x) to_lds(lds + x * NT * 16, p + x * RPX * pitch, off[x % NV]);
+        } else {
+            int here = tid;                      // (formed here: held over the loop it would be spilled)
+            asm volatile("" : "+v"(here));
+#pragma unroll
+            for (int x = 0; x < PT; ++x) {
+                const int row = here / CH + x * RPX, c = here % CH;
+                to_lds(lds + x * NT * 16, base + (int64_t)min(max(r0 + row, 0), nk - 1) * pitch + piece(row, c) * 16);
+            }
         }
     };
+    // Keys run a step ahead of the values: while the exponentials of one step keep the vector unit busy, the matrix cores form the logits
+    // of the next.  A tile of keys therefore begins AHEAD rows behind the tile of values.
+    auto bring_keys = [&](int t, int buf) { bring_rows(t * BK + AHEAD, Kh, krow, klds + buf * BK * RB, koff, key_piece); };
+    auto bring_values = [&](int t, int buf) { bring_rows(t * BK, Vh, vrow, vlds + buf * BK * RB, voff, value_piece); };
 
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.0f);
     float m = -INFINITY, l = 0.0f;
+    f32x16 s[SB];                                // logits of the step that is next to be summed
+
+    // Logits of the blocks from key j on, divided by sc.  The bias is where the products begin (in fp32, which would feel the roundings of
+    // sums around a far key's bias, it is added behind them).
+    auto logits = [&](const char* kt, int j, f32x16(&x)[SB]) {
+        const float base = slope * (float)(j + half * 4 - pos);
+#pragma unroll
+        for (int c = 0; c < SB; ++c) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[c][r] = BIAS && EB == 2 ? fmaf(slope, (float)(c * 32 + (r >> 2) * 8 + (r & 3)), base) : 0.0f;
+#pragma unroll
+            for (int g = 0; g < KS; ++g) {
+                const uint4 k = *(const uint4*)(kt + (c * 32 + n0) * RB + key_piece(n0, 2 * g + half) * 16);
+                x[c] = Mma<T>::group(k, __builtin_bit_cast(uint4, q[g]), x[c]);
+            }
+            if constexpr (BIAS && EB == 4) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[c][r] = fmaf(slope, (float)(c * 32 + (r >> 2) * 8 + (r & 3)), base) + x[c][r];
+            }
+        }
+    };
+    auto masked = [&](f32x16(&x)[SB], int j) {
+#pragma unroll
+        for (int c = 0; c < SB; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[c][r] = j + half * 4 + c * 32 + (r >> 2) * 8 + (r & 3) > pos ? -INFINITY : x[c][r];
+    };
+    const float sc = a.sc;
+    auto largest = [&](const f32x16(&x)[SB]) {
+        float top = x[0][0];
+#pragma unroll
+        for (int c = 0; c < SB; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[c][r]);
+        return half_max(top) * sc;
+    };
+    // the reference, where the largest exponent asks for it
+    auto raise = [&](float top) {
+        if (__any(top > m + kAttendSlack || m == -INFINITY)) {
+            const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : hw_exp2(m - to);
+            m = to;
+            l *= by;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] *= by;
+        }
+    };
+    // Operand x of the values, rows i * 32 .. of it: of 16 lanes each four bring 16 neighbouring elements of a key, and a lane
+    // receives its element of the four keys.  In fp32 four products take one key of either half each.
+    auto values = [&](const char* vt, int x, int i) {
+        if constexpr (EB == 2) {
+            const int row = x * 16 + half * 4 + (lane >> 2 & 3), c = i * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + row * RB + value_piece(row, c) * 16 + (lane & 1) * 8));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (row + 8) * RB + value_piece(row + 8, c) * 16 + (lane & 1) * 8));
+            const uint2 u = __builtin_bit_cast(uint2, lo), v = __builtin_bit_cast(uint2, hi);
+            return make_uint4(u.x, u.y, v.x, v.y);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int row = x * 8 + half * 4 + y, byte = (i * 32 + n0) * 4;
+                w[y] = *(const uint32_t*)(vt + row * RB + value_piece(row, byte / 16) * 16 + byte % 16);
+            }
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    };
+    constexpr int XS = EB == 2 ? 2 : 4, PX = 16 / XS;  // operands of 32 keys, terms of each
+    // One step: its exponentials beside the next one's logits, then its values beside the next one's largest.
+    auto step = [&](const char* next, const char* vt, int j, bool edge) {
+        f32x16 y[SB];
+        logits(next, j + AHEAD, y);
+        const float ref = m == -INFINITY ? 0.0f : m;
+        uint4 p[SB][XS];
+#pragma unroll
+        for (int c = 0; c < SB; ++c) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[c][r] = hw_exp2(fmaf(s[c][r], sc, -ref));
+#pragma unroll
+            for (int r = 0; r < 16; ++r) l += s[c][r];
+#pragma unroll
+            for (int x = 0; x < XS; ++x) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (EB == 2) w[e] = pack_pair<T>(s[c][x * PX + 2 * e], s[c][x * PX + 2 * e + 1]);
+                    else w[e] = __float_as_uint(s[c][x * PX + e]);
+                }
+                asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // here, beside the products, and not behind the branch
+                p[c][x] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        if (edge) {
+            asm volatile("");                    // a branch: the comparisons would be a fifth of a block's vector work
+            masked(y, j + AHEAD);
+        }
+#pragma unroll
+        for (int c = 0; c < SB; ++c)
+#pragma unroll
+            for (int x = 0; x < XS; ++x)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[i] = Mma<T>::group(values(vt, c * XS + x, i), p[c][x], o[i]);
+        const float top = largest(y);
+        raise(top);
+#pragma unroll
+        for (int c = 0; c < SB; ++c) s[c] = y[c];
+    };
 
     if (t0 < t1) {
         if (tid == 0) bad_s = 0;
-        bring(t1 - 1);
+        bring_keys(t0 - 1, 1);
+        bring_keys(t0, 0);
+        bring_values(t0, 0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        park(t1 - 1, (t1 - 1) & 1);
-        __syncthreads();
+        logits(kbuf[1] + (BK - AHEAD + wk * SB * 32) * RB, t0 * BK + wk * SB * 32, s);
+        masked(s, t0 * BK + wk * SB * 32);
+        raise(largest(s));
     }
-    for (int t = t1 - 1; t >= t0; --t) {         // from the diagonal
-        const int buf = t & 1;
-        if (t > t0) bring(t - 1);
-        if (t * BK <= last) {                    // else the wave's rows see nothing of it
-            const char* kt = kbuf[buf] + n0 * RB;
-            f32x16 s[NB];
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile is there, and nobody reads the other buffers any more
+        __syncthreads();
+        if (t + 1 < t1) {
+            bring_keys(t + 1, buf ^ 1);
+            bring_values(t + 1, buf ^ 1);
+        }
+        if (t * BK + BK - 1 > lowest) {          // some row does not see all of the tile: see the end
+            bool bad = false;
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb) {
-                s[kb] = (f32x16)(0.0f);
-#pragma unroll
-                for (int g = 0; g < KS; ++g) {
-                    const uint4 k = *(const uint4*)(kt + kb * 32 * RB + key_piece(n0, 2 * g + half) * 16);
-                    s[kb] = Mma<T>::group(k, __builtin_bit_cast(uint4, q[g]), s[kb]);
-                }
+            for (int x = 0; x < PT; ++x) {
+                u32x4_t* at = (u32x4_t*)(vbuf[buf] + (tid + x * NT) * 16);
+                u32x4_t v = *at;
+                if (clean_piece<T>(v)) *at = v, bad = true;
             }
-            const int key0 = t * BK + half * 4;
-            float sc = a.sc;
-            if constexpr (BIAS) {
-                const float base = slope * (float)(key0 - pos);
+            if (bad) bad_s = 1;
+            __syncthreads();
+        }
+        if (t * BK > last) continue;             // the wave's rows see nothing of it
+        const bool edge = (t + 1) * BK + AHEAD - 1 > first;
+#pragma unroll 1
+        for (int u = 0; u < US; ++u) {
+            const int row = (u * WK + wk) * SB * 32;
+            step(kbuf[buf] + row * RB, vbuf[buf] + row * RB, t * BK + row, edge);
+        }
+    }
+    __syncthreads();
+    const bool bad = t0 < t1 && bad_s;
+    if constexpr (WK > 1) {                      // the waves that share rows
+        if (wk > 0) {
+            float4* w = (float4*)(lds + ((wk - 1) * WR + wr) * (D * 32 * 4 + 512));
 #pragma unroll
-                for (int kb = 0; kb < NB; ++kb)
+            for (int i = 0; i < DT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kb][r] = fmaf(s[kb][r], a.sc, fmaf(slope, (float)(kb * 32 + (r >> 2) * 8 + (r & 3)), base));
-                sc = 1.0f;
-            }
-            if (t * BK + BK - 1 > first) {
+                for (int y = 0; y < 4; ++y) w[(i * 4 + y) * 64 + lane] = make_float4(o[i][4 * y], o[i][4 * y + 1], o[i][4 * y + 2], o[i][4 * y + 3]);
+            ((float2*)(w + DT * 256))[lane] = make_float2(m, l);
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll 1
+        for (int c = 0; c < WK - 1; ++c) {
+            const float4* w = (const float4*)(lds + (c * WR + wr) * (D * 32 * 4 + 512));
+            const float2 ml = ((const float2*)(w + DT * 256))[lane];
+            const float to = fmaxf(m, ml.x), ref = to == -INFINITY ? 0.0f : to, mine_by = hw_exp2(m - ref), by = hw_exp2(ml.x - ref);
+            m = to;
+            l = fmaf(by, ml.y, l * mine_by);
 #pragma unroll
-                for (int kb = 0; kb < NB; ++kb)
+            for (int i = 0; i < DT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kb][r] = key0 + kb * 32 + (r >> 2) * 8 + (r & 3) > pos ? -INFINITY : s[kb][r];
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
-            top = half_max(top) * sc;
-            if (__any(top > m + kAttendSlack || m == -INFINITY)) {
-                const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : hw_exp2(m - to);
-                m = to;
-                l *= by;
-#pragma unroll
-                for (int i = 0; i < DT; ++i) o[i] *= by;
-            }
-            const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kb][r] = hw_exp2(BIAS ? s[kb][r] - ref : fmaf(s[kb][r], sc, -ref));
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) l += s[kb][r];
-            const char* vt = vbuf[buf];
-            // Operand x of the values, rows i * 32 .. of it: of 16 lanes each four bring 16 neighbouring elements of a key, and a lane
-            // receives its element of the four keys.  In fp32 four products take one key of either half each.
-            auto values = [&](int x, int i) {
-                if constexpr (EB == 2) {
-                    const int row = x * 16 + half * 4 + (lane >> 2 & 3), c = i * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + row * RB + value_piece(row, c) * 16 + (lane & 1) * 8));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (row + 8) * RB + value_piece(row + 8, c) * 16 + (lane & 1) * 8));
-                    const uint2 u = __builtin_bit_cast(uint2, lo), v = __builtin_bit_cast(uint2, hi);
-                    return make_uint4(u.x, u.y, v.x, v.y);
-                } else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int row = x * 8 + half * 4 + y, byte = (i * 32 + n0) * 4;
-                        w[y] = *(const uint32_t*)(vt + row * RB + value_piece(row, byte / 16) * 16 + byte % 16);
-                    }
-                    return make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            };
-            constexpr int XS = EB == 2 ? 2 : 4, PX = 16 / XS;  // operands of 32 keys, terms of each
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-                for (int x = 0; x < XS; ++x) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        if constexpr (EB == 2) w[y] = pack_pair<T>(s[kb][x * PX + 2 * y], s[kb][x * PX + 2 * y + 1]);
-                        else w[y] = __float_as_uint(s[kb][x * PX + y]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < DT; ++i) o[i] = Mma<T>::group(values(kb * XS + x, i), make_uint4(w[0], w[1], w[2], w[3]), o[i]);
+                for (int y = 0; y < 4; ++y) {
+                    const float4 v = w[(i * 4 + y) * 64 + lane];
+                    o[i][4 * y] = fmaf(by, v.x, o[i][4 * y] * mine_by);
+                    o[i][4 * y + 1] = fmaf(by, v.y, o[i][4 * y + 1] * mine_by);
+                    o[i][4 * y + 2] = fmaf(by, v.z, o[i][4 * y + 2] * mine_by);
+                    o[i][4 * y + 3] = fmaf(by, v.w, o[i][4 * y + 3] * mine_by);
                 }
         }
-        if (t > t0) park(t - 1, buf ^ 1);
-        __syncthreads();
     }
     l = half_sum(l);
     if (!mine) return;
-    if (t0 < t1 && bad_s) {
+    if (bad) {
         // 0 times an infinity would reach the rows that do not see it: such values were left out of the products with tiles of which
         // some rows do not see all, and go to the rows that do here
 #pragma unroll 1
@@ -330,13 +436,30 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
     }
 }
 
-constexpr int kAttendWaves = 4;
+// Shapes of a workgroup, by the bytes of a row: many rows; fewer; a few.
+template <int RB>
+struct AttendShapes {
+    using Many = AttendShape<4, 1, RB == 256 ? 2 : 1, 2>;
+    using Fewer = AttendShape<2, 2, 1, 2>;
+    using Few = AttendShape<1, 4, 1, 4>;
+};
+template <>
+struct AttendShapes<512> {
+    using Many = AttendShape<4, 1, 1, 1>;
+    using Fewer = AttendShape<2, 2, 1, 2>;
+    using Few = AttendShape<2, 2, 1, 2>;
+};
 
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
-    a->tiles = (int32_t)(((int64_t)a->n * a->G + kAttendWaves * 32 - 1) / (kAttendWaves * 32));
+    const int64_t units = (int64_t)a->B * a->H, rows = (int64_t)a->n * a->G;
+    const bool wide = d * (dtype == KF_F32 ? 4 : 2) > 256;
+    const int64_t slots = wide ? 256 : 512;      // workgroups that the chip holds at once
+    a->shape = units * ((rows + 127) / 128) >= 2 * slots ? 0 : units * ((rows + 63) / 64) >= slots / 2 || wide ? 1 : 2;
+    a->block_rows = a->shape == 0 ? 128 : a->shape == 1 || wide ? 64 : 32;
+    a->tiles = (int32_t)((rows + a->block_rows - 1) / a->block_rows);
     a->S = 1;
-    const int64_t blocks = (int64_t)a->B * a->H * a->tiles;
-    const int32_t keys = d * (dtype == KF_F32 ? 4 : 2) > 256 ? 32 : 64, walk = (a->m + keys - 1) / keys;
+    const int64_t blocks = units * a->tiles;
+    const int64_t walk = ((int64_t)a->m + 127) / 128;
     if (blocks < 256) {
         int64_t S = 512 / blocks;
         if (S > walk / 4) S = walk / 4;
@@ -344,16 +467,23 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
         if (S > 1) a->S = (int32_t)S;
     }
     a->blocks = blocks * a->S;
-    a->ws_rows = a->S > 1 ? (int64_t)a->B * a->H * a->tiles * kAttendWaves * 32 : 0;
+    a->ws_rows = a->S > 1 ? blocks * a->block_rows : 0;
 }
 
+template <typename T, int D, typename SHAPE>
+static void launch_attend_s(const AttendArgs& a, hipStream_t st) {
+    const int64_t run = (a.blocks + kXcds - 1) / kXcds;
+    const dim3 grid((unsigned)(run * kXcds)), block(SHAPE::WR * SHAPE::WK * kWave);
+    if (a.slopes) hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, false>), grid, block, 0, st, a);
+}
 template <typename T, int D>
 static hipError_t launch_attend_d(const AttendArgs& a, hipStream_t st) {
-    const int64_t run = (a.blocks + kXcds - 1) / kXcds;
-    const dim3 grid((unsigned)(run * kXcds)), block(kAttendWaves * kWave);
-    if (a.slopes) hipLaunchKernelGGL((attend_kernel<T, D, kAttendWaves, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attend_kernel<T, D, kAttendWaves, false>), grid, block, 0, st, a);
-    if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * kAttendWaves * 32);
+    using S = AttendShapes<D * (int)sizeof(T)>;
+    if (a.shape == 0) launch_attend_s<T, D, typename S::Many>(a, st);
+    else if (a.shape == 1) launch_attend_s<T, D, typename S::Fewer>(a, st);
+    else launch_attend_s<T, D, typename S::Few>(a, st);
+    if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * a.block_rows);
     return hipGetLastError();
 }
 

@@ -322,6 +322,7 @@ struct AttendArgs {
     int32_t B, n, m, H, G;
     float sc;                // |scale| * log2(e); the queries take the scale's sign, or zero with it
     uint32_t q_keep, q_flip;
+    int32_t shape, block_rows;  // of a workgroup: many rows, fewer, a few
     int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys
     int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
     float* ws_o;             // [ws_rows][S][d]

@@ -32,7 +32,7 @@ def test_prompt_refusals():
                 dict(q_stride=(-8, 512, 128)), dict(k_stride=(2560, 516, 128)), dict(out_stride=(8, 8, 4)), dict(q_start=0x5000, seq_n=0x6000),
                 dict(k_start=0x5000, seq_m=0x6000), dict(n=1 << 30, q_per_kv=2), dict(H=1 << 24, q_per_kv=2)):
         expect(binding.KF_EINVAL, call, **bad)
-    for bad in (dict(d=96), dict(dtype=kf.F32, d=256), dict(B=1 << 20, H=1 << 14)):
+    for bad in (dict(d=96), dict(dtype=kf.F32, d=256), dict(B=1 << 20, H=1 << 14), dict(k_stride=(0, 128, (1 << 26) + 8))):
         expect(binding.KF_EUNSUPPORTED, call, **bad)
     for bad in (None, (0x100000, 64), (0x100004, 1 << 40)):
         expect(binding.KF_EWORKSPACE, call, workspace=bad)
