@@ -360,7 +360,14 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
     __syncthreads();
     const int64_t tile = 64 * D, to = ((int64_t)l * a.pages + a.table[(int64_t)b * a.max_pages + blockIdx.x]) * a.H + h;
     const int64_t layer = (int64_t)l * a.pages;
-    constexpr int CH = D / 16, PT = 64 * CH / kPageThreads;
+    constexpr int CH = D / 16, PT = 64 * CH / kPageThreads, ROWS = D / kPageWaves;  // rows of values of a wave
+    uint8_t vc[ROWS];
+    const int vpage = page_s[lane];
+    {
+        const uint8_t* from = a.V + ((layer + max(vpage, 0)) * a.H + h) * tile + (int64_t)wv * ROWS * 64 + slot_s[lane];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) vc[r] = from[r * 64];
+    }
     {
         uint4 c[PT];
         float most = 0.0f;
@@ -400,13 +407,10 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
         if (tid == 0) a.k_scale[to] = power_of_two(e);
     }
     {
-        constexpr int ROWS = D / kPageWaves;  // of a wave
         uint8_t c[ROWS];
-        const int page = page_s[lane];
         const float s = vs_s[lane];
-        const uint8_t* from = a.V + ((layer + max(page, 0)) * a.H + h) * tile + (int64_t)wv * ROWS * 64 + slot_s[lane];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) c[r] = page < 0 ? 0 : from[r * 64];
+        for (int r = 0; r < ROWS; ++r) c[r] = vpage < 0 ? 0 : vc[r];
         float most = 0.0f;
 #pragma unroll
         for (int r = 0; r < ROWS; r += 4) {
@@ -459,19 +463,23 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
     }
     const int s0 = max(first - j * 64, 0), s1 = min(len - j * 64, 64);  // slots of the new rows
     const int64_t at = ((int64_t)l * a.pages + page) * a.H + h;
+    uint4 rows[2][PT];
 #pragma unroll
     for (int tensor = 0; tensor < 2; ++tensor) {
         const T* src = (const T*)(tensor ? a.v : a.k) + (((int64_t)lb * a.H + h) * a.rows + (j * 64 - first)) * D;  // row of slot 0
-        uint8_t* dst = (tensor ? a.V : a.K) + at * 64 * D;
-        float* scale = (tensor ? a.v_scale : a.k_scale) + at;
-        uint4 r[PT];
-        float most = 0.0f;
 #pragma unroll
         for (int x = 0; x < PT; ++x) {
             const int p = tid + x * kPageThreads, t = p / CH;
-            r[x] = make_uint4(0u, 0u, 0u, 0u);
-            if (t >= s0 && t < s1) r[x] = stream_load((const uint4*)(src + t * D) + p % CH);
+            rows[tensor][x] = make_uint4(0u, 0u, 0u, 0u);
+            if (t >= s0 && t < s1) rows[tensor][x] = stream_load((const uint4*)(src + t * D) + p % CH);
         }
+    }
+#pragma unroll
+    for (int tensor = 0; tensor < 2; ++tensor) {
+        uint8_t* dst = (tensor ? a.V : a.K) + at * 64 * D;
+        float* scale = (tensor ? a.v_scale : a.k_scale) + at;
+        const uint4(&r)[PT] = rows[tensor];
+        float most = 0.0f;
 #pragma unroll
         for (int x = 0; x < PT; ++x) {
             float f[8];
@@ -674,24 +682,42 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
         }
     }
 
-    for (int j = p0 + wv; j < p1; j += kPageWaves) {
-        const int page = __builtin_amdgcn_readfirstlane(table[j]);
-        if ((unsigned)page >= (unsigned)a.pages) {  // there is no such page: its tokens are left out
+    // A page's keys are asked for when the last one's are used up, its values likewise: a wave has half a page or a page under way always.
+    uint4 k[4][C], v[DT];
+    float ks = 0.0f, vs = 0.0f;
+    int page = -1;
+    const uint32_t klane = ((n0 >> 2) * 16 + (n0 & 3)) * D + g * 16, vlane = n0 * 64 + g * 16;
+    auto find = [&](int j) {                     // a number that is no page's leaves the page's tokens out, and page 0 is read
+        page = j < p1 ? __builtin_amdgcn_readfirstlane(table[j]) : -1;
+        if (j < p1 && (unsigned)page >= (unsigned)a.pages) {
             if (lane == 0) count_error(a);
-            continue;
+            page = -1;
         }
-        const int64_t at = ((int64_t)l * a.pages + page) * a.H + h;
-        const uint8_t* kp = a.K + at * 64 * D + ((n0 >> 2) * 16 + (n0 & 3)) * D + g * 16;
-        const uint8_t* vp = a.V + at * 64 * D + n0 * 64 + g * 16;
-        uint4 k[4][C], v[DT];
+    };
+    auto bring_keys = [&]() {
+        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
+        const uint8_t* kp = a.K + at * 64 * D + klane;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int c = 0; c < C; ++c) k[t][c] = stream_load((const uint4*)(kp + t * 4 * D + c * 64));
+        ks = a.k_scale[at] * a.sc;
+    };
+    auto bring_values = [&]() {
+        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
+        const uint8_t* vp = a.V + at * 64 * D + vlane;
 #pragma unroll
         for (int i = 0; i < DT; ++i) v[i] = stream_load((const uint4*)(vp + i * 16 * 64));
-        const float ks = a.k_scale[at] * a.sc, vs = a.v_scale[at];
-
+        vs = a.v_scale[at];
+    };
+    find(p0 + wv);
+    if (p0 + wv < p1) {
+        bring_keys();
+        bring_values();
+    }
+    for (int j = p0 + wv; j < p1; j += kPageWaves) {
+        const int live = page < 0 ? 0 : old;     // tokens that are there
+        const float kby = ks, vby = vs;
         p_f4_t x[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -702,20 +728,22 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
                 x[t] = code_product<T>(k[t][c].z, k[t][c].w, q[2 * c + 1], x[t]);
             }
         }
+        find(j + kPageWaves);
+        if (j + kPageWaves < p1) bring_keys();
         const int j0 = j * 64 + g * 16;          // token of x[t][r]: j0 + 4 t + r
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if constexpr (BIAS) x[t][r] = fmaf(x[t][r], ks, slope * (float)(j0 + 4 * t + r - old));
-                else x[t][r] *= ks;
+                if constexpr (BIAS) x[t][r] = fmaf(x[t][r], kby, slope * (float)(j0 + 4 * t + r - old));
+                else x[t][r] *= kby;
             }
-        if (j * 64 + 64 > old) {                 // the last page: slots that hold no token of this sequence, or the new one's
+        if (j * 64 + 64 > live) {                // the last page: slots that hold no token of this sequence, or the new one's
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = j0 + 4 * t + r < old ? x[t][r] : -INFINITY;
-            const int have = max(min(old - j0, 16), 0);
+                for (int r = 0; r < 4; ++r) x[t][r] = j0 + 4 * t + r < live ? x[t][r] : -INFINITY;
+            const int have = max(min(live - j0, 16), 0);
             uint32_t mask[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) mask[i] = have - 4 * i >= 4 ? ~0u : have - 4 * i <= 0 ? 0u : (1u << 8 * (have - 4 * i)) - 1u;
@@ -754,8 +782,9 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
             y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].x, v[i].y), p[0], y, 0, 0, 0);
             y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].z, v[i].w), p[1], y, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[i][r] = fmaf(y[r], vs, o[i][r]);
+            for (int r = 0; r < 4; ++r) o[i][r] = fmaf(y[r], vby, o[i][r]);
         }
+        if (j + kPageWaves < p1) bring_values();
     }
 
     sum = across_sum(sum);
@@ -797,27 +826,42 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
     }
 }
 
-// Joins a unit's splits: a workgroup a unit, its threads the elements of its heads.
-__global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs a, int D) {
-    const unsigned u = blockIdx.x;
+// Joins the splits of a unit's head: D / 4 threads take a row of sums, the groups of them every so many-th split.
+constexpr int kPageMaxSplits = 256;
+template <int D>
+__global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs a) {
+    constexpr int LANES = D / 4, GROUPS = kPageThreads / LANES;
+    __shared__ float by_s[kPageMaxSplits];
+    __shared__ float red[kPageWaves];
+    __shared__ float4 part[GROUPS][LANES];
+    const unsigned u = blockIdx.x / (unsigned)a.G;
+    const int y = (int)(blockIdx.x - u * (unsigned)a.G), tid = threadIdx.x, grp = tid / LANES, e = tid % LANES;
     const int b = (int)(u / (unsigned)a.H % (unsigned)a.B), n = a.len[b];
     if ((a.seq_n && a.seq_n[b] != 1) || n < 1 || n > (int64_t)a.max_pages * 64) return;
     const int parts = min(((n - 1) >> 6) / a.chunk, a.S - 1) + 1;
-    for (int i = threadIdx.x; i < a.G * D; i += kPageThreads) {
-        const int y = i / D;
-        const int64_t at = (int64_t)u * a.S * a.G + y;
-        float top = -INFINITY;
-        for (int s = 0; s < parts; ++s) top = fmaxf(top, a.ws_ml[at + s * a.G].x);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, v = 0.0f;
-        for (int s = 0; s < parts; ++s) {
-            const float2 ml = a.ws_ml[at + s * a.G];
-            const float by = hw_exp2(ml.x - ref);
-            sum = fmaf(by, ml.y, sum);
-            v = fmaf(by, a.ws_o[(at + s * a.G) * D + (i - y * D)], v);
-        }
-        a.out[(int64_t)u * a.G * D + i] = sum == 0.0f ? 0.0f : v / sum;
+    const int64_t at = (int64_t)u * a.S * a.G + y;
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    if (tid < parts) ml = a.ws_ml[at + (int64_t)tid * a.G];
+    const float top = block_max<kPageThreads>(ml.x, red), by = hw_exp2(ml.x - (top == -INFINITY ? 0.0f : top));
+    if (tid < parts) by_s[tid] = by;
+    const float sum = block_sum<kPageThreads>(tid < parts ? by * ml.y : 0.0f, red);
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int s = grp; s < parts; s += GROUPS) {
+        const float4 x = ((const float4*)(a.ws_o + (at + (int64_t)s * a.G) * D))[e];
+        const float w = by_s[s];
+        v.x = fmaf(w, x.x, v.x), v.y = fmaf(w, x.y, v.y), v.z = fmaf(w, x.z, v.z), v.w = fmaf(w, x.w, v.w);
     }
+    part[grp][e] = v;
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int s = 1; s < GROUPS; ++s) {
+        const float4 x = part[s][e];
+        v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    ((float4*)(a.out + ((int64_t)u * a.G + y) * D))[e] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
 }
 
 // ---------------------------------------------------------------- launches
@@ -826,6 +870,7 @@ int32_t page_most_splits(int64_t U, int32_t max_pages) {
     int64_t S = (1024 + U - 1) / U;
     const int64_t most = (max_pages + kPageWaves - 1) / kPageWaves;
     if (S > most) S = most;
+    if (S > kPageMaxSplits) S = kPageMaxSplits;
     return (int32_t)(S < 1 ? 1 : S);
 }
 void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint) {
@@ -840,7 +885,7 @@ static void launch_step_d(const PageArgs& a, int64_t U, hipStream_t st) {
     const dim3 grid((unsigned)(U * a.S)), block(kPageThreads);
     if (a.slopes) hipLaunchKernelGGL((page_step_kernel<T, D, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((page_step_kernel<T, D, false>), grid, block, 0, st, a);
-    if (a.S > 1) hipLaunchKernelGGL(page_join_kernel, dim3((unsigned)U), block, 0, st, a, D);
+    if (a.S > 1) hipLaunchKernelGGL((page_join_kernel<D>), dim3((unsigned)(U * a.G)), block, 0, st, a);
 }
 template <typename T, int D>
 static void launch_write_d(const PageArgs& a, hipStream_t st) {
