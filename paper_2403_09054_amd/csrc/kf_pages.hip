@@ -19,6 +19,8 @@ namespace kf {
 
 constexpr int kPageThreads = 256;
 constexpr int kPageWaves = kPageThreads / kWave;
+constexpr int kStepWaves = 4;
+constexpr int kStepThreads = kStepWaves * kWave;
 constexpr int kTableThreads = 1024;
 
 typedef __bf16 p_bf2_t __attribute__((ext_vector_type(2)));
@@ -621,29 +623,67 @@ __device__ __forceinline__ void page_append(const T* row, uint8_t* dst, float* s
 
 // blockIdx.x = unit * S + split, unit = (layer * B + row) * H + head.  A split is a.chunk pages, shared out to the waves.
 template <typename T, int D, bool BIAS>
-__global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs a) {
+__global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs a) {
     constexpr int C = D / 64, NQ = D / 32, DT = D / 16;
-    __shared__ float o_s[kPageWaves][8][D];
-    __shared__ float m_s[kPageWaves][8], l_s[kPageWaves][8];
+    __shared__ float o_s[kStepWaves][8][D];
+    __shared__ float m_s[kStepWaves][8], l_s[kStepWaves][8];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 15, g = lane >> 4;
     const unsigned u = blockIdx.x / (unsigned)a.S;
     const int split = (int)(blockIdx.x - u * (unsigned)a.S);
     const unsigned lb = u / (unsigned)a.H;
     const int h = (int)(u - lb * (unsigned)a.H), l = (int)(lb / (unsigned)a.B), b = (int)(lb - (unsigned)l * (unsigned)a.B);
-    const int n = a.len[b];
-    const bool asked = !a.seq_n || a.seq_n[b] == 1, there = n >= 1 && n <= (int64_t)a.max_pages * 64;
+    // a wave's first page is looked up beside the length that says whether it is one
+    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    const int p0 = split * a.chunk;
+    const int n = uniform_load(a.len + b), ask = a.seq_n ? uniform_load(a.seq_n + b) : 1;
+    int ahead = uniform_load(table + min(p0 + wv, a.max_pages - 1));
+    const bool asked = ask == 1, there = n >= 1 && n <= (int64_t)a.max_pages * 64;
     float* out = a.out + (int64_t)u * a.G * D;
     if (!asked || !there) {
         if (split == 0) {
-            for (int i = tid; i < a.G * D; i += kPageThreads) out[i] = 0.0f;
+            for (int i = tid; i < a.G * D; i += kStepThreads) out[i] = 0.0f;
             if (asked && tid == 0) count_error(a);
         }
         return;
     }
     const int old = n - 1, tail = old >> 6, owner = min(tail / a.chunk, a.S - 1);
     if (split > owner) return;
-    const int p0 = split * a.chunk, p1 = split == owner ? tail + ((old & 63) != 0) : p0 + a.chunk;
-    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    const int p1 = split == owner ? tail + ((old & 63) != 0) : p0 + a.chunk;
+
+    // A page's keys are asked for when the last one's are used up, its values likewise: a wave has half a page or a page under way always.
+    uint4 k[4][C], v[DT];
+    float ks = 0.0f, vs = 0.0f;
+    int page = -1;
+    const uint32_t klane = ((n0 >> 2) * 16 + (n0 & 3)) * D + g * 16, vlane = n0 * 64 + g * 16;
+    auto find = [&](int j) {                     // a number that is no page's leaves the page's tokens out, and page 0 is read
+        page = ahead;
+        if (j < p1 && (unsigned)page >= (unsigned)a.pages) {
+            if (lane == 0) count_error(a);
+            page = -1;
+        }
+        ahead = uniform_load(table + min(j + kStepWaves, a.max_pages - 1));
+    };
+    auto bring_keys = [&]() {
+        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
+        const uint8_t* kp = a.K + at * 64 * D + klane;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < C; ++c) k[t][c] = stream_load((const uint4*)(kp + t * 4 * D + c * 64));
+        ks = uniform_load(a.k_scale + at) * a.sc;
+    };
+    auto bring_values = [&]() {
+        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
+        const uint8_t* vp = a.V + at * 64 * D + vlane;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) v[i] = stream_load((const uint4*)(vp + i * 16 * 64));
+        vs = uniform_load(a.v_scale + at);
+    };
+    find(p0 + wv);
+    if (p0 + wv < p1) {
+        bring_keys();
+        bring_values();
+    }
 
     const int head = n0 & 7, part = n0 >> 3;     // of this lane's column
     uint4 q[NQ];
@@ -663,12 +703,11 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
     const T* vn = (const T*)a.v + (int64_t)u * D;
     if (split == owner && wv == 0) {             // the token itself: row 0 of a tile
         p_f4_t x = p_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        uint4 row[NQ];
 #pragma unroll
-        for (int c = 0; c < NQ; ++c) {
-            uint4 k = make_uint4(0u, 0u, 0u, 0u);
-            if (n0 == 0) k = *(const uint4*)(kn + g * 16 + (c >> 1) * 64 + (c & 1) * 8);
-            x = key_product<T>(k, q[c], x);
-        }
+        for (int c = 0; c < NQ; ++c) row[c] = *(const uint4*)(kn + g * 16 + (c >> 1) * 64 + (c & 1) * 8);
+#pragma unroll
+        for (int c = 0; c < NQ; ++c) x = key_product<T>(n0 == 0 ? row[c] : make_uint4(0u, 0u, 0u, 0u), q[c], x);
         m = __shfl(x[0], n0, kWave) * a.sc;
         const float p = hw_exp2(m - (m == -INFINITY ? 0.0f : m) + kPageLift);
         sum = g == 0 ? p : 0.0f;
@@ -682,40 +721,7 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
         }
     }
 
-    // A page's keys are asked for when the last one's are used up, its values likewise: a wave has half a page or a page under way always.
-    uint4 k[4][C], v[DT];
-    float ks = 0.0f, vs = 0.0f;
-    int page = -1;
-    const uint32_t klane = ((n0 >> 2) * 16 + (n0 & 3)) * D + g * 16, vlane = n0 * 64 + g * 16;
-    auto find = [&](int j) {                     // a number that is no page's leaves the page's tokens out, and page 0 is read
-        page = j < p1 ? __builtin_amdgcn_readfirstlane(table[j]) : -1;
-        if (j < p1 && (unsigned)page >= (unsigned)a.pages) {
-            if (lane == 0) count_error(a);
-            page = -1;
-        }
-    };
-    auto bring_keys = [&]() {
-        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
-        const uint8_t* kp = a.K + at * 64 * D + klane;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int c = 0; c < C; ++c) k[t][c] = stream_load((const uint4*)(kp + t * 4 * D + c * 64));
-        ks = a.k_scale[at] * a.sc;
-    };
-    auto bring_values = [&]() {
-        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
-        const uint8_t* vp = a.V + at * 64 * D + vlane;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) v[i] = stream_load((const uint4*)(vp + i * 16 * 64));
-        vs = a.v_scale[at];
-    };
-    find(p0 + wv);
-    if (p0 + wv < p1) {
-        bring_keys();
-        bring_values();
-    }
-    for (int j = p0 + wv; j < p1; j += kPageWaves) {
+    for (int j = p0 + wv; j < p1; j += kStepWaves) {
         const int live = page < 0 ? 0 : old;     // tokens that are there
         const float kby = ks, vby = vs;
         p_f4_t x[4];
@@ -728,8 +734,8 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
                 x[t] = code_product<T>(k[t][c].z, k[t][c].w, q[2 * c + 1], x[t]);
             }
         }
-        find(j + kPageWaves);
-        if (j + kPageWaves < p1) bring_keys();
+        find(j + kStepWaves);
+        if (j + kStepWaves < p1) bring_keys();
         const int j0 = j * 64 + g * 16;          // token of x[t][r]: j0 + 4 t + r
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -784,7 +790,7 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[i][r] = fmaf(y[r], vby, o[i][r]);
         }
-        if (j + kPageWaves < p1) bring_values();
+        if (j + kStepWaves < p1) bring_values();
     }
 
     sum = across_sum(sum);
@@ -797,15 +803,15 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
         }
     if (lane < 8) m_s[wv][lane] = m, l_s[wv][lane] = sum;
     __syncthreads();
-    for (int i = tid; i < a.G * D; i += kPageThreads) {
+    for (int i = tid; i < a.G * D; i += kStepThreads) {
         const int y = i / D, d = i - y * D;
         float top = m_s[0][y];
 #pragma unroll
-        for (int w = 1; w < kPageWaves; ++w) top = fmaxf(top, m_s[w][y]);
+        for (int w = 1; w < kStepWaves; ++w) top = fmaxf(top, m_s[w][y]);
         const float ref = top == -INFINITY ? 0.0f : top;
         float s = 0.0f, v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kPageWaves; ++w) {
+        for (int w = 0; w < kStepWaves; ++w) {
             const float by = hw_exp2(m_s[w][y] - ref);
             s = fmaf(by, l_s[w][y], s);
             v = fmaf(by, o_s[w][y][d], v);
@@ -818,7 +824,7 @@ __global__ void __launch_bounds__(kPageThreads) page_step_kernel(const PageArgs 
         }
     }
     if (split == owner && wv < 2) {              // every wave is done with the page
-        const int page = table[tail];
+        const int page = uniform_load(table + tail);
         if ((unsigned)page < (unsigned)a.pages) {
             const int64_t at = ((int64_t)l * a.pages + page) * a.H + h;
             page_append<T, D>(wv ? vn : kn, (wv ? a.V : a.K) + at * 64 * D, (wv ? a.v_scale : a.k_scale) + at, old & 63, wv != 0, lane);
@@ -868,7 +874,7 @@ __global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs 
 // Splits of a unit's pages: a page a wave at least, and as many workgroups as fill the chip twice.
 int32_t page_most_splits(int64_t U, int32_t max_pages) {
     int64_t S = (1024 + U - 1) / U;
-    const int64_t most = (max_pages + kPageWaves - 1) / kPageWaves;
+    const int64_t most = (max_pages + kStepWaves - 1) / kStepWaves;
     if (S > most) S = most;
     if (S > kPageMaxSplits) S = kPageMaxSplits;
     return (int32_t)(S < 1 ? 1 : S);
@@ -882,10 +888,10 @@ void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint) {
 
 template <typename T, int D>
 static void launch_step_d(const PageArgs& a, int64_t U, hipStream_t st) {
-    const dim3 grid((unsigned)(U * a.S)), block(kPageThreads);
+    const dim3 grid((unsigned)(U * a.S)), block(kStepThreads);
     if (a.slopes) hipLaunchKernelGGL((page_step_kernel<T, D, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((page_step_kernel<T, D, false>), grid, block, 0, st, a);
-    if (a.S > 1) hipLaunchKernelGGL((page_join_kernel<D>), dim3((unsigned)(U * a.G)), block, 0, st, a);
+    if (a.S > 1) hipLaunchKernelGGL((page_join_kernel<D>), dim3((unsigned)(U * a.G)), dim3(kPageThreads), 0, st, a);
 }
 template <typename T, int D>
 static void launch_write_d(const PageArgs& a, hipStream_t st) {
