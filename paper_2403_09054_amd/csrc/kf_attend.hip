@@ -72,6 +72,8 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
+constexpr int kFarTile = 128;        // keys whose largest norm is kept
+constexpr float kAttendFar = 48.0f;  // all the keys that are left out together weigh less than 2^-24 of a row
 // A reference is raised once a row's largest exponent is this far above it; terms stay below 2^8.
 constexpr float kAttendSlack = 8.0f;
 
@@ -87,16 +89,32 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     char(*const kbuf)[BK * RB] = (char(*)[BK * RB]) lds;
     char(*const vbuf)[BK * RB] = kbuf + 2;
+    __shared__ float2 far_s[BIAS ? W : 1];
     __shared__ int bad_s;                        // a tile of which some rows do not see all holds a value that is infinite or no number
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 31, half = lane >> 5;
     const int wr = wv % WR, wk = wv / WR;
 
-    // an XCD takes a run of neighbouring workgroups: those of one cached head share its L2
-    const unsigned run = (gridDim.x + kXcds - 1) / kXcds, at = blockIdx.x % kXcds * run + blockIdx.x / kXcds;
-    if (at >= (unsigned)a.blocks) return;
-    const unsigned per = (unsigned)(a.tiles * a.S), unit = at / per, rest = at - unit * per;
+    // The workgroups of a cached head share an XCD and its L2.  Where the heads are a multiple of the XCDs each takes its share of every
+    // sequence's, to and fro and another share for the next sequence, the last heads first: what a position bias leaves them to do grows
+    // with their number.  Else an XCD takes a run of neighbouring workgroups.
+    const unsigned per = (unsigned)(a.tiles * a.S), xcd = blockIdx.x % kXcds, place = blockIdx.x / kXcds;
+    unsigned rest;
+    int b, h;
+    if (a.H % kXcds == 0) {
+        const unsigned local = place / per, back = local / (unsigned)a.B, r = (unsigned)a.H / kXcds - 1 - back;
+        rest = place - local * per;
+        b = (int)(local - back * (unsigned)a.B);
+        const unsigned x = (xcd + (unsigned)b) % kXcds;
+        h = (int)(r * kXcds + (r & 1 ? kXcds - 1 - x : x));
+    } else {
+        const unsigned at = xcd * (gridDim.x / kXcds) + place;
+        if (at >= (unsigned)a.blocks) return;
+        rest = at % per;
+        b = (int)(at / per / (unsigned)a.H);
+        h = (int)(at / per - (unsigned)b * (unsigned)a.H);
+    }
+    const unsigned unit = (unsigned)b * (unsigned)a.H + (unsigned)h;
     const int qt = a.tiles - 1 - (int)(rest / (unsigned)a.S), split = (int)(rest % (unsigned)a.S);  // long walks first
-    const int h = (int)(unit / (unsigned)a.B), b = (int)(unit % (unsigned)a.B);
 
     int64_t q0 = 0, k0 = 0;
     int nq = a.n, nk = a.m;
@@ -127,9 +145,40 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     // tiles: the workgroup's rows see keys [0, kend)
     const int kend = min(nk, off + min(R0 + ROWS - 1, rows - 1) / a.G + 1);
     int t0 = 0, t1 = kend > 0 ? (kend + BK - 1) / BK : 0;
+    if constexpr (BIAS) {
+        // Far keys that cannot matter.  A row's largest logit is at least its own key's, -sc |q| |k_own|; one at distance D is at most
+        // sc |q| |k| - slope D: where that lies 2^-kAttendFar below for every row, a tile of keys is left out, with all before it.  (A tile
+        // that holds a value which is no number, or infinite, has an infinite norm, and NaN compares as it should.)
+        if (a.ws_kn && t1 > 0) {
+            float qq = 0.0f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qq = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, q[s]), qq);
+            qq = wave_max(half_sum(qq));
+            const float flat = -wave_max(-slope);
+            if (lane == 0) far_s[wv] = make_float2(qq, flat);
+            __syncthreads();
+            float2 all = far_s[0];
+#pragma unroll
+            for (int w = 1; w < W; ++w) all = make_float2(fmaxf(all.x, far_s[w].x), fminf(all.y, far_s[w].y));
+            const int lowest = off + R0 / a.G, count = (a.m + kFarTile - 1) / kFarTile;
+            const float* kn = a.ws_kn + (int64_t)unit * count;
+            const float qn = sqrtf(all.x) * a.sc, own = fmaxf(kn[max(lowest, 0) / kFarTile], kn[(kend - 1) / kFarTile]);
+            int from = lowest > 0 ? lowest / kFarTile : 0;  // tiles that end before the lowest row
+            for (int i = 0; i < from; i += kWave) {
+                const int tile = i + lane;
+                const bool far = tile < from && qn * (kn[min(tile, from - 1)] + own) - all.y * a.sc * (float)(lowest - (tile * kFarTile + kFarTile - 1)) < -kAttendFar;
+                const uint64_t no = __ballot(!far);
+                if (no) {
+                    from = min(from, i + __builtin_ctzll(no));
+                    break;
+                }
+            }
+            t0 = __builtin_amdgcn_readfirstlane(from) * kFarTile / BK;
+        }
+    }
     if (a.S > 1) {
-        const int each = (t1 + a.S - 1) / a.S;
-        t0 = min(split * each, t1);
+        const int each = (t1 - t0 + a.S - 1) / a.S;
+        t0 = min(t0 + split * each, t1);
         t1 = min(t0 + each, t1);
     }
     const int first = off + min(R0 + wr * 32, rows - 1) / a.G;  // of the wave
@@ -397,14 +446,50 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
         }
 }
 
+// Largest norm of kFarTile keys, or infinity where a key or a value among them is infinite or no number: blockIdx = (tile, unit).
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attend_norms_kernel(const AttendArgs a) {
+    constexpr int CH = D * (int)sizeof(T) / 16, RPX = 256 / CH;
+    __shared__ float red[4];
+    const int b = blockIdx.y / a.H, h = blockIdx.y - b * a.H, tid = threadIdx.x;
+    int64_t k0 = 0;
+    int nk = a.m;
+    if (a.k_start) k0 = a.k_start[b], nk = (int)min((int64_t)a.k_start[b + 1] - k0, (int64_t)0x7fffffff);
+    else if (a.seq_m) nk = a.seq_m[b];
+    if (nk < 0 || nk > a.m || k0 < 0) return;    // no such sequence
+    const T* Kh = (const T*)a.K + (a.k_start ? k0 * a.k_st : b * a.k_sb) + h * a.k_sh + tid % CH * (16 / (int)sizeof(T));
+    const T* Vh = (const T*)a.V + (a.k_start ? k0 * a.v_st : b * a.v_sb) + h * a.v_sh + tid % CH * (16 / (int)sizeof(T));
+    uint4 k[kFarTile / RPX], v[kFarTile / RPX];
+#pragma unroll
+    for (int x = 0; x < kFarTile / RPX; ++x) {
+        const int row = blockIdx.x * kFarTile + tid / CH + x * RPX;
+        k[x] = v[x] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < nk) {
+            k[x] = *(const uint4*)(Kh + row * a.k_st);
+            v[x] = *(const uint4*)(Vh + row * a.v_st);
+        }
+    }
+    float most = 0.0f;
+#pragma unroll
+    for (int x = 0; x < kFarTile / RPX; ++x) {
+        float d = dot_piece<T>(k[x], k[x], 0.0f);
+#pragma unroll
+        for (int o = 1; o < CH; o <<= 1) d += __shfl_xor(d, o, kWave);
+        u32x4_t w = {v[x].x, v[x].y, v[x].z, v[x].w};
+        most = fmaxf(most, clean_piece<T>(w) || !(d < INFINITY) ? INFINITY : d);
+    }
+    most = block_max<256>(most, red);
+    if (tid == 0) a.ws_kn[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sqrtf(most);
+}
+
 // Joins the parts of a row: one wave a row, a lane takes D / 64 elements.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int rows_pad) {
     constexpr int E = D / 64;
     const int lane = threadIdx.x & 63;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), unit = at / rows_pad;
-    const int R = (int)(at - unit * rows_pad), h = (int)(unit / a.B), b = (int)(unit % a.B);
-    if (h >= a.H) return;
+    const int R = (int)(at - unit * rows_pad), b = (int)(unit / a.H), h = (int)(unit % a.H);
+    if (b >= a.B) return;
     int64_t q0 = 0, k0 = 0;
     int nq = a.n, nk = a.m;
     if (a.q_start) q0 = a.q_start[b], nq = (int)min((int64_t)a.q_start[b + 1] - q0, (int64_t)0x7fffffff);
@@ -467,6 +552,8 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
         if (S > 1) a->S = (int32_t)S;
     }
     a->blocks = blocks * a->S;
+    // A row of far tiles is looked for where a key is read often enough: the search reads K and V once more.
+    a->far_tiles = a->slopes && (int64_t)a->n * a->G >= 2048 && units <= 65535 ? (a->m + kFarTile - 1) / kFarTile : 0;
     a->ws_rows = a->S > 1 ? blocks * a->block_rows : 0;
 }
 
@@ -480,6 +567,8 @@ static void launch_attend_s(const AttendArgs& a, hipStream_t st) {
 template <typename T, int D>
 static hipError_t launch_attend_d(const AttendArgs& a, hipStream_t st) {
     using S = AttendShapes<D * (int)sizeof(T)>;
+    if (a.far_tiles)
+        hipLaunchKernelGGL((attend_norms_kernel<T, D>), dim3((unsigned)a.far_tiles, (unsigned)(a.B * a.H)), dim3(256), 0, st, a);
     if (a.shape == 0) launch_attend_s<T, D, typename S::Many>(a, st);
     else if (a.shape == 1) launch_attend_s<T, D, typename S::Fewer>(a, st);
     else launch_attend_s<T, D, typename S::Few>(a, st);

@@ -324,9 +324,11 @@ struct AttendArgs {
     uint32_t q_keep, q_flip;
     int32_t shape, block_rows;  // of a workgroup: many rows, fewer, a few
     int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys
+    int32_t far_tiles;       // of a cached head, whose norms tell what a position bias rules out; 0: not looked for
     int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
     float* ws_o;             // [ws_rows][S][d]
     float2* ws_ml;           // [ws_rows][S] reference and sum
+    float* ws_kn;            // [B*H][far_tiles], or NULL
 };
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype);
 hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream);
