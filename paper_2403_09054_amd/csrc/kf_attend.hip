@@ -73,7 +73,7 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 
 constexpr int kFarTile = 128;        // keys whose largest norm is kept
-constexpr float kAttendFar = 48.0f;  // all the keys that are left out together weigh less than 2^-24 of a row
+constexpr float kAttendFar = 40.0f;  // 65536 keys that are left out weigh less than 2^-24 of a row together
 // A reference is raised once a row's largest exponent is this far above it; terms stay below 2^8.
 constexpr float kAttendSlack = 8.0f;
 
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     char(*const kbuf)[BK * RB] = (char(*)[BK * RB]) lds;
     char(*const vbuf)[BK * RB] = kbuf + 2;
-    __shared__ float2 far_s[BIAS ? W : 1];
+    __shared__ float4 far_s[BIAS ? W : 1];
     __shared__ int bad_s;                        // a tile of which some rows do not see all holds a value that is infinite or no number
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 31, half = lane >> 5;
     const int wr = wv % WR, wk = wv / WR;
@@ -146,27 +146,38 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     const int kend = min(nk, off + min(R0 + ROWS - 1, rows - 1) / a.G + 1);
     int t0 = 0, t1 = kend > 0 ? (kend + BK - 1) / BK : 0;
     if constexpr (BIAS) {
-        // Far keys that cannot matter.  A row's largest logit is at least its own key's, -sc |q| |k_own|; one at distance D is at most
-        // sc |q| |k| - slope D: where that lies 2^-kAttendFar below for every row, a tile of keys is left out, with all before it.  (A tile
-        // that holds a value which is no number, or infinite, has an infinite norm, and NaN compares as it should.)
+        // Far keys that cannot matter.  A row's largest logit is at least its own key's; one at distance D is at most sc |q| |k| - slope D:
+        // where that lies kAttendFar below for every row, a tile of keys is left out, with all before it.  (A tile that holds a value which
+        // is no number, or infinite, has an infinite norm; what is no number makes no row's bound hold.)
         if (a.ws_kn && t1 > 0) {
-            float qq = 0.0f;
+            float qq = 0.0f, own = 0.0f;
+            const char* mine = Kh + (int64_t)min(max(pos, 0), nk - 1) * krow + half * 16;
+            u32x4_t k[KS];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qq = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, q[s]), qq);
-            qq = wave_max(half_sum(qq));
+            for (int s = 0; s < KS; ++s) k[s] = *(const u32x4_t*)(mine + s * 32);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                qq = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, q[s]), qq);
+                own = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, k[s]), own);
+            }
+            qq = half_sum(qq);
+            own = half_sum(own);
+            const bool odd = __any(!(qq < INFINITY) || !(fabsf(own) < INFINITY));
+            qq = odd ? INFINITY : wave_max(qq);
+            own = wave_max(-own);
             const float flat = -wave_max(-slope);
-            if (lane == 0) far_s[wv] = make_float2(qq, flat);
+            if (lane == 0) far_s[wv] = make_float4(qq, flat, own, 0.0f);
             __syncthreads();
-            float2 all = far_s[0];
+            float4 all = far_s[0];
 #pragma unroll
-            for (int w = 1; w < W; ++w) all = make_float2(fmaxf(all.x, far_s[w].x), fminf(all.y, far_s[w].y));
+            for (int w = 1; w < W; ++w) all.x = fmaxf(all.x, far_s[w].x), all.y = fminf(all.y, far_s[w].y), all.z = fmaxf(all.z, far_s[w].z);
             const int lowest = off + R0 / a.G, count = (a.m + kFarTile - 1) / kFarTile;
             const float* kn = a.ws_kn + (int64_t)unit * count;
-            const float qn = sqrtf(all.x) * a.sc, own = fmaxf(kn[max(lowest, 0) / kFarTile], kn[(kend - 1) / kFarTile]);
+            const float qn = sqrtf(all.x);
             int from = lowest > 0 ? lowest / kFarTile : 0;  // tiles that end before the lowest row
             for (int i = 0; i < from; i += kWave) {
                 const int tile = i + lane;
-                const bool far = tile < from && qn * (kn[min(tile, from - 1)] + own) - all.y * a.sc * (float)(lowest - (tile * kFarTile + kFarTile - 1)) < -kAttendFar;
+                const bool far = tile < from && a.sc * (qn * kn[min(tile, from - 1)] + all.z - all.y * (float)(lowest - (tile * kFarTile + kFarTile - 1))) < -kAttendFar;
                 const uint64_t no = __ballot(!far);
                 if (no) {
                     from = min(from, i + __builtin_ctzll(no));
