@@ -1121,8 +1121,8 @@ kf_status kf_page_write(const kf_pages* p, const void* k, const void* v, int32_t
     if (!k || !v) return fail(KF_EINVAL, "k and v must not be NULL");
     if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(KF_EINVAL, "k and v must be 16-byte aligned");
     if (n < 1 || (rows != 0 && rows < n)) return fail(KF_EINVAL, "n=%d must be positive and not above rows=%d", n, rows);
-    if ((int64_t)p->L * p->B > 65535 || p->H > 65535)
-        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads exceed the largest launch", p->L, p->B, p->H);
+    if ((int64_t)p->L * p->B * p->H * (((int64_t)n + 62) / 64 + 1) > kMaxGrid)
+        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads of %d rows exceed the largest launch", p->L, p->B, p->H, n);
     a.k = k;
     a.v = v;
     a.n = n;
@@ -1182,8 +1182,8 @@ kf_status kf_page_compact(const kf_pages* p, const int32_t* keep, int32_t k, con
     if (!keep) return fail(KF_EINVAL, "keep is NULL");
     const int64_t room = (int64_t)p->max_pages * KF_PAGE_TOKENS;
     if (k < 1 || k > room) return fail(KF_EINVAL, "k=%d outside [1, %lld]", k, (long long)room);
-    if ((int64_t)p->L * p->B > 65535 || p->H > 65535)
-        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads exceed the largest launch", p->L, p->B, p->H);
+    if ((int64_t)p->L * p->B * p->H * ((k + 63) / 64) > kMaxGrid - 8)
+        return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads of %d tokens exceed the largest launch", p->L, p->B, p->H, k);
     a.keep = keep;
     a.kept = k;
     a.which = which;

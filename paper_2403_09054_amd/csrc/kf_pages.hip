@@ -333,15 +333,19 @@ __global__ void __launch_bounds__(kTableThreads) page_shrink_kernel(const PageAr
 // ---------------------------------------------------------------- kept rows into new pages
 __device__ __forceinline__ float block_most(float v, float* red) { return block_max<kPageThreads>(v, red); }
 
-// blockIdx = (new page, head, layer * B + row).  Keys: 16-byte pieces of rows.  Values: a wave's lanes are the page's tokens, a load a
+// A workgroup a new page of a head.  Keys: 16-byte pieces of rows.  Values: a wave's lanes are the page's tokens, a load a
 // byte of each; a sequence's tokens are in order, so that a load falls on few lines.
 template <int D>
 __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs a) {
     __shared__ int page_s[64], slot_s[64];
     __shared__ float ks_s[64], vs_s[64];
     __shared__ float red[kPageWaves];
+    __shared__ __attribute__((aligned(16))) uint8_t turn_s[kPageWaves][D / kPageWaves * 64];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int lb = blockIdx.z, l = lb / a.B, b = lb - l * a.B, h = blockIdx.y, j0 = blockIdx.x * 64;
+    // neighbouring workgroups take neighbouring heads, whose tiles lie side by side in a page
+    const unsigned pages = (unsigned)(a.kept + 63) / 64, rest = blockIdx.x / (unsigned)a.H;
+    const int h = (int)(blockIdx.x - rest * (unsigned)a.H), lb = (int)(rest / pages), j = (int)(rest - (unsigned)lb * pages);
+    const int l = lb / a.B, b = lb - l * a.B, j0 = j * 64;
     const int n = a.ws_copy[b].x;
     if (n == 0) return;
     const int live = min(64, a.kept - j0);
@@ -360,7 +364,7 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
         vs_s[tid] = page < 0 ? 0.0f : a.v_scale[((int64_t)l * a.pages + page) * a.H + h];
     }
     __syncthreads();
-    const int64_t tile = 64 * D, to = ((int64_t)l * a.pages + a.table[(int64_t)b * a.max_pages + blockIdx.x]) * a.H + h;
+    const int64_t tile = 64 * D, to = ((int64_t)l * a.pages + a.table[(int64_t)b * a.max_pages + j]) * a.H + h;
     const int64_t layer = (int64_t)l * a.pages;
     constexpr int CH = D / 16, PT = 64 * CH / kPageThreads, ROWS = D / kPageWaves;  // rows of values of a wave
     uint8_t vc[ROWS];
@@ -423,25 +427,33 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
         }
         const int e = page_exponent(block_most(most, red));
         const float inv = power_of_two(-e);
-        uint8_t* w = a.V + to * tile + (int64_t)wv * ROWS * 64 + lane;
-        if (lane < live) {
+        // by way of the wave's own LDS: 16 tokens of a row a store
+        uint8_t* turn = turn_s[wv];
 #pragma unroll
-            for (int r = 0; r < ROWS; r += 4) {
-                float f[4];
-                decode4(c[r] | c[r + 1] << 8 | c[r + 2] << 16 | (uint32_t)c[r + 3] << 24, f);
-                const uint32_t v = encode4(f[0] * s, f[1] * s, f[2] * s, f[3] * s, inv);
-                w[r * 64] = (uint8_t)v;
-                w[r * 64 + 64] = (uint8_t)(v >> 8);
-                w[r * 64 + 128] = (uint8_t)(v >> 16);
-                w[r * 64 + 192] = (uint8_t)(v >> 24);
-            }
+        for (int r = 0; r < ROWS; r += 4) {
+            float f[4];
+            decode4(c[r] | c[r + 1] << 8 | c[r + 2] << 16 | (uint32_t)c[r + 3] << 24, f);
+            const uint32_t v = encode4(f[0] * s, f[1] * s, f[2] * s, f[3] * s, inv);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn[(r + i) * 64 + lane] = (uint8_t)(v >> (8 * i));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        uint8_t* w = a.V + to * tile + (int64_t)wv * ROWS * 64;
+#pragma unroll
+        for (int x = 0; x < ROWS / 16; ++x) {
+            const int p = x * kWave + lane, t = p % 4 * 16;
+            if (t + 16 <= live) *(uint4*)(w + p * 16) = *(const uint4*)(turn + p * 16);
+            else
+                for (int i = t; i < live; ++i) w[p * 16 + i - t] = turn[p * 16 + i - t];
         }
         if (tid == 0) a.v_scale[to] = power_of_two(e);
     }
 }
 
 // ---------------------------------------------------------------- rows into pages
-// blockIdx = (page behind the first that the call touches, head, layer * B + row).  A thread holds 16-byte pieces of the page's new rows;
+// blockIdx.x = (layer * B + row, page behind the first that the call touches, head), the head fastest.  A thread holds 16-byte pieces of the page's new rows;
 // values are turned in LDS.
 template <typename T, int D>
 __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs a) {
@@ -449,13 +461,15 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
     __shared__ __attribute__((aligned(16))) uint8_t turn[D * PITCH];
     __shared__ float red[kPageWaves];
     const int tid = threadIdx.x;
-    const int lb = blockIdx.z, l = lb / a.B, b = lb - l * a.B, h = blockIdx.y;
+    const unsigned pages = (unsigned)(a.n + 62) / 64 + 1, rest = blockIdx.x / (unsigned)a.H;
+    const int h = (int)(blockIdx.x - rest * (unsigned)a.H), lb = (int)(rest / pages), jx = (int)(rest - (unsigned)lb * pages);
+    const int l = lb / a.B, b = lb - l * a.B;
     const int add = a.seq_n ? a.seq_n[b] : a.n, len = a.len[b];
     if (add < 1 || add > a.n) return;
     const bool none = len < add || len > (int64_t)a.max_pages * 64;
-    const int first = len - add, j = (first >> 6) + blockIdx.x;
+    const int first = len - add, j = (first >> 6) + jx;
     if (none || (int64_t)j * 64 >= len) {
-        if (none && blockIdx.x == 0 && tid == 0) count_error(a);  // no room was reserved for these rows
+        if (none && jx == 0 && tid == 0) count_error(a);  // no room was reserved for these rows
         return;
     }
     const int page = a.table[(int64_t)b * a.max_pages + j];
@@ -895,7 +909,8 @@ static void launch_step_d(const PageArgs& a, int64_t U, hipStream_t st) {
 }
 template <typename T, int D>
 static void launch_write_d(const PageArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((a.n + 62) / 64 + 1), (unsigned)a.H, (unsigned)(a.L * a.B)), block(kPageThreads);
+    const int64_t blocks = ((int64_t)(a.n + 62) / 64 + 1) * a.H * a.L * a.B;
+    const dim3 grid((unsigned)blocks), block(kPageThreads);
     hipLaunchKernelGGL((page_write_kernel<T, D>), grid, block, 0, st, a);
 }
 
@@ -943,7 +958,8 @@ hipError_t launch_page_fork(const PageArgs& a, int32_t d, hipStream_t st) {
 }
 hipError_t launch_page_compact(const PageArgs& a, int32_t d, hipStream_t st) {
     hipLaunchKernelGGL(page_shrink_kernel, dim3(1), dim3(kTableThreads), (size_t)a.B * 4, st, a);
-    const dim3 grid((unsigned)((a.kept + 63) / 64), (unsigned)a.H, (unsigned)(a.L * a.B)), block(kPageThreads);
+    const int64_t blocks = (int64_t)((a.kept + 63) / 64) * a.H * a.L * a.B;
+    const dim3 grid((unsigned)blocks), block(kPageThreads);
     if (d == 64) hipLaunchKernelGGL((page_keep_kernel<64>), grid, block, 0, st, a);
     else if (d == 128) hipLaunchKernelGGL((page_keep_kernel<128>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((page_keep_kernel<256>), grid, block, 0, st, a);

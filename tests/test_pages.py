@@ -63,8 +63,8 @@ def test_page_refusals_of_one_call():
     expect(binding.KF_EINVAL, CALLS["fork"], fake(), parent=None)
     for bad in (dict(keep=None), dict(k=0), dict(k=20 * P + 1)):
         expect(binding.KF_EINVAL, CALLS["compact"], fake(), **bad)
-    for name in ("write", "compact"):
-        expect(binding.KF_EUNSUPPORTED, CALLS[name], fake(L=1 << 15, B=4, H=4))
+    expect(binding.KF_EUNSUPPORTED, CALLS["write"], fake(L=1 << 15, B=4, H=64), n=1 << 20)
+    expect(binding.KF_EUNSUPPORTED, CALLS["compact"], fake(L=1 << 15, B=4, H=64, max_pages=1 << 20), k=1 << 20)
     assert kf.kf_page_workspace_bytes(fake(d=96)) == 0 < kf.kf_page_workspace_bytes(fake())
     expect(binding.KF_EUNSUPPORTED, kf.new_page_workspace, fake(d=96), device="cpu")
 
