@@ -131,9 +131,23 @@ __device__ __forceinline__ void take_pages(const PageArgs& a, int* need, uint32_
     __syncthreads();
 }
 
-// Gives up every page that row b of the table names (a wave).
-__device__ __forceinline__ void release_row(const PageArgs& a, const int32_t* row, int lane) {
-    for (int j = lane; j < a.max_pages; j += kWave) {
+// The rows of the table are shared out to teams of threads, as many as a row has pages, at most a wave: a launch of one workgroup is a
+// chain of trips to memory, and what few rows ask for goes in one trip.
+struct Team {
+    int shift, first, step, lane;  // log2 of its threads; its first row, rows between two of its own; this thread's place
+    __device__ __forceinline__ Team(int max_pages) {
+        shift = 0;
+        while ((1 << shift) < max_pages && shift < 6) ++shift;
+        first = threadIdx.x >> shift;
+        step = kTableThreads >> shift;
+        lane = threadIdx.x & ((1 << shift) - 1);
+    }
+    __device__ __forceinline__ int size() const { return 1 << shift; }
+};
+
+// Gives up every page that a row of the table names (`size` threads).
+__device__ __forceinline__ void release_row(const PageArgs& a, const int32_t* row, int lane, int size) {
+    for (int j = lane; j < a.max_pages; j += size) {
         const int p = row[j];
         if ((unsigned)p < (unsigned)a.pages) atomicSub(a.refs + p, 1);
         else if (p != -1) count_error(a);
@@ -159,18 +173,19 @@ __global__ void __launch_bounds__(kTableThreads) page_reserve_kernel(const PageA
     }
     __syncthreads();
     take_pages(a, need, red);
-    // a wave a sequence
-    const int lane = tid & 63;
-    for (int b = tid >> 6; b < a.B; b += kTableThreads / 64) {
+    const Team team(a.max_pages);
+    const int lane = team.lane;
+    for (int b = team.first; b < a.B; b += team.step) {
         int len, add;
         const int k = asks(b, &len, &add);
+        __builtin_amdgcn_wave_barrier();         // (the length is read by all of the team before it is written)
         if (k < 0 || add == 0) continue;
         if (k > 0 && need[b] < 0) {
             if (lane == 0) count_error(a);
             continue;
         }
         const int have = pages_of(len);
-        for (int j = lane; j < k; j += kWave) {
+        for (int j = lane; j < k; j += team.size()) {
             const int p = a.ws_list[need[b] + j];
             a.table[(int64_t)b * a.max_pages + have + j] = p;
             a.refs[p] = 1;
@@ -183,7 +198,7 @@ __global__ void __launch_bounds__(kPageThreads) page_free_kernel(const PageArgs 
     const int b = blockIdx.x * kPageWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (b >= a.B || (a.which && a.which[b] == 0)) return;
     int32_t* row = a.table + (int64_t)b * a.max_pages;
-    release_row(a, row, lane);
+    release_row(a, row, lane, kWave);
     for (int j = lane; j < a.max_pages; j += kWave) row[j] = -1;
     if (lane == 0) a.len[b] = 0;
 }
@@ -191,67 +206,85 @@ __global__ void __launch_bounds__(kPageThreads) page_free_kernel(const PageArgs 
 // Rows that go on as another row's do: their pages are released, the parent's full ones shared, and a page taken for its last where that
 // is not full; what is to be copied goes to ws_copy.
 __global__ void __launch_bounds__(kTableThreads) page_fork_kernel(const PageArgs a) {
-    extern __shared__ int need[];  // [B]
+    extern __shared__ int need[];  // [B]; first the parent, -1: the row stays as it is, -2: it comes out empty
     __shared__ uint32_t red[kTableThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int tid = threadIdx.x;
     const int64_t room = (int64_t)a.max_pages * 64;
-    // the parent, or -1: row b stays as it is
-    auto from = [&](int b) {
+    const Team team(a.max_pages);
+    const int lane = team.lane;
+    for (int b = tid; b < a.B; b += kTableThreads) {
         const int p = a.which[b];
-        return p == b || (unsigned)p >= (unsigned)a.B || a.which[p] != p || a.len[p] < 0 || a.len[p] > room ? -1 : p;
-    };
-    for (int b = wv; b < a.B; b += kTableThreads / 64) {
-        const int p = from(b);
-        if (p < 0) {
-            if (lane == 0) {
-                if (a.which[b] != b) count_error(a);
-                need[b] = 0;
-                a.ws_copy[b] = make_int2(-1, -1);
+        int from = -1;
+        if (p != b) {
+            if ((unsigned)p < (unsigned)a.B) {
+                const int further = a.which[p], n = a.len[p];
+                if (further == p && n >= 0 && n <= room) from = p;
             }
+            if (from < 0) count_error(a);
+        }
+        need[b] = from;
+    }
+    __syncthreads();
+    for (int b = team.first; b < a.B; b += team.step) {
+        const int p = need[b];
+        if (p < 0) continue;
+        const int32_t* theirs = a.table + (int64_t)p * a.max_pages;
+        const int many = pages_of(a.len[p]);
+        for (int j = lane; j < many; j += team.size())
+            if ((unsigned)theirs[j] >= (unsigned)a.pages) need[b] = -2;  // the parent's row names a page that there is not
+    }
+    __syncthreads();
+    for (int b = team.first; b < a.B; b += team.step) {
+        const int p = need[b];
+        if (p == -1) {
+            if (lane == 0) a.ws_copy[b] = make_int2(-1, -1);
             continue;
         }
         int32_t* row = a.table + (int64_t)b * a.max_pages;
-        const int32_t* theirs = a.table + (int64_t)p * a.max_pages;
-        const int n = a.len[p], full = n >> 6;
-        release_row(a, row, lane);
-        bool bad = false;  // the parent's row names a page that there is not
-        for (int j = lane; j < pages_of(n); j += kWave) bad |= (unsigned)theirs[j] >= (unsigned)a.pages;
-        bad = __any(bad);
-        for (int j = lane; j < a.max_pages; j += kWave) {
-            const bool share = !bad && j < full;
-            if (share) atomicAdd(a.refs + theirs[j], 1);
-            row[j] = share ? theirs[j] : -1;
+        const int32_t* theirs = a.table + (int64_t)max(p, 0) * a.max_pages;
+        const int n = p < 0 ? 0 : a.len[p], full = n >> 6;
+        for (int j = lane; j < a.max_pages; j += team.size()) {
+            const int old = row[j], share = j < full ? theirs[j] : -1;
+            if ((unsigned)old < (unsigned)a.pages) atomicSub(a.refs + old, 1);
+            else if (old != -1) count_error(a);
+            if (share >= 0) atomicAdd(a.refs + share, 1);
+            row[j] = share;
         }
         if (lane == 0) {
-            if (bad) count_error(a);
-            need[b] = !bad && (n & 63) ? 1 : 0;
-            a.ws_copy[b] = make_int2(bad ? -2 : (n & 63) ? theirs[full] : -1, -1);  // -2: comes out empty
+            if (p < 0) count_error(a);
+            // the page to copy; -3: no page more, -2: comes out empty
+            a.ws_copy[b] = make_int2(p < 0 ? -2 : (n & 63) ? theirs[full] : -3, p);
         }
     }
     __threadfence();
     __syncthreads();
+    for (int b = tid; b < a.B; b += kTableThreads) need[b] = a.ws_copy[b].x >= 0;
+    __syncthreads();
     take_pages(a, need, red);
-    for (int b = wv; b < a.B; b += kTableThreads / 64) {
-        const int p = from(b);
-        if (p < 0) continue;
-        int32_t* row = a.table + (int64_t)b * a.max_pages;
-        const int n = a.len[p], full = n >> 6;
-        const int src = a.ws_copy[b].x;
-        if (src == -2) {
-            if (lane == 0) a.len[b] = 0, a.ws_copy[b] = make_int2(-1, -1);
-        } else if (src >= 0 && need[b] < 0) {  // no page left: it comes out empty
-            release_row(a, row, lane);
-            for (int j = lane; j < a.max_pages; j += kWave) row[j] = -1;
-            if (lane == 0) count_error(a), a.len[b] = 0, a.ws_copy[b] = make_int2(-1, -1);
-        } else if (lane == 0) {
-            if (src >= 0) {
-                const int to = a.ws_list[need[b]];
-                row[full] = to;
-                a.refs[to] = 1;
-                a.ws_copy[b] = make_int2(src, to);
+    for (int b = tid; b < a.B; b += kTableThreads) {
+        const int2 c = a.ws_copy[b];
+        if (c.x == -1) continue;
+        const int n = c.x == -2 ? 0 : a.len[c.y];
+        int2 copy = make_int2(-1, -1);
+        if (c.x >= 0) {
+            if (need[b] < 0) {                   // no page left: it comes out empty
+                count_error(a);
+                int32_t* row = a.table + (int64_t)b * a.max_pages;
+                for (int j = 0; j < (n >> 6); ++j) {
+                    atomicSub(a.refs + row[j], 1);
+                    row[j] = -1;
+                }
+                a.len[b] = 0;
+                a.ws_copy[b] = copy;
+                continue;
             }
-            a.len[b] = n;
+            const int to = a.ws_list[need[b]];
+            a.table[(int64_t)b * a.max_pages + (n >> 6)] = to;
+            a.refs[to] = 1;
+            copy = make_int2(c.x, to);
         }
+        a.len[b] = n;
+        a.ws_copy[b] = copy;
     }
 }
 
@@ -285,48 +318,58 @@ __global__ void __launch_bounds__(kPageThreads) page_copy_kernel(const PageArgs 
 __global__ void __launch_bounds__(kTableThreads) page_shrink_kernel(const PageArgs a) {
     extern __shared__ int need[];  // [B]
     __shared__ uint32_t red[kTableThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int tid = threadIdx.x;
     const int64_t room = (int64_t)a.max_pages * 64;
-    const int want = pages_of(a.kept);
-    for (int b = wv; b < a.B; b += kTableThreads / 64) {
-        const int n = a.len[b];
-        bool go = (!a.which || a.which[b] != 0) && n > a.kept;
-        if (go) {
-            const int32_t* row = a.table + (int64_t)b * a.max_pages;
-            bool bad = n > room;
-            if (!bad)
-                for (int j = lane; j < pages_of(n); j += kWave) bad |= (unsigned)row[j] >= (unsigned)a.pages;
-            if (__any(bad)) {
-                if (lane == 0) count_error(a);
-                go = false;
-            }
-        }
-        if (lane == 0) need[b] = go ? want : 0;
+    const Team team(a.max_pages);
+    const int lane = team.lane, want = pages_of(a.kept);
+    for (int b = tid; b < a.B; b += kTableThreads) {
+        const int n = a.len[b], on = a.which ? a.which[b] : 1;
+        const bool go = on != 0 && n > a.kept;
+        need[b] = go ? n > room ? -1 : want : 0;
+        a.ws_copy[b] = make_int2(go ? n : 0, 0);
     }
     __syncthreads();
-    // who asked: its own word, since a place may be 0
-    for (int b = tid; b < a.B; b += kTableThreads) a.ws_copy[b] = make_int2(need[b] > 0 ? a.len[b] : 0, 0);
+    for (int b = team.first; b < a.B; b += team.step) {
+        if (need[b] <= 0) continue;
+        const int32_t* row = a.table + (int64_t)b * a.max_pages;
+        const int many = pages_of(a.len[b]);
+        for (int j = lane; j < many; j += team.size())
+            if ((unsigned)row[j] >= (unsigned)a.pages) need[b] = -1;
+    }
+    __syncthreads();
+    for (int b = tid; b < a.B; b += kTableThreads)
+        if (need[b] < 0) {
+            count_error(a);
+            need[b] = 0;
+            a.ws_copy[b] = make_int2(0, 0);
+        }
     __syncthreads();
     take_pages(a, need, red);
-    for (int b = wv; b < a.B; b += kTableThreads / 64) {
-        if (a.ws_copy[b].x == 0) continue;
-        if (need[b] < 0) {
-            if (lane == 0) count_error(a), a.ws_copy[b] = make_int2(0, 0);
-            continue;
+    for (int b = tid; b < a.B; b += kTableThreads)
+        if (a.ws_copy[b].x != 0) {
+            if (need[b] < 0) {
+                count_error(a);
+                a.ws_copy[b] = make_int2(0, 0);
+            } else a.len[b] = a.kept;
         }
+    __threadfence_block();
+    __syncthreads();
+    for (int b = team.first; b < a.B; b += team.step) {
+        if (a.ws_copy[b].x == 0) continue;
         int32_t* row = a.table + (int64_t)b * a.max_pages;
         int32_t* old = a.ws_old + (int64_t)b * a.max_pages;
-        release_row(a, row, lane);
-        for (int j = lane; j < a.max_pages; j += kWave) {
-            old[j] = row[j];
+        for (int j = lane; j < a.max_pages; j += team.size()) {
+            const int had = row[j];
             int p = -1;
             if (j < want) {
                 p = a.ws_list[need[b] + j];
                 a.refs[p] = 1;
             }
+            if ((unsigned)had < (unsigned)a.pages) atomicSub(a.refs + had, 1);
+            else if (had != -1) count_error(a);
+            old[j] = had;
             row[j] = p;
         }
-        if (lane == 0) a.len[b] = a.kept;
     }
 }
 
