@@ -1004,7 +1004,9 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     kf::plan_attend(a, p->d, p->dtype);
     if (a->blocks > kMaxGrid - 8) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
     *sums = align_up((size_t)a->ws_rows * a->S * p->d * 4, 256);
-    *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256) + align_up((size_t)a->far_tiles * p->B * p->H * 4, 256);
+    // records and their references, parts, far tiles
+    *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256) + align_up((size_t)a->ws_rows / a->block_rows * 4, 256) +
+             align_up((size_t)a->far_tiles * p->B * p->H * 4, 256);
     return KF_OK;
 }
 
@@ -1030,7 +1032,10 @@ kf_status kf_prompt_attend(const kf_prompt* p, const void* Q, const void* K, con
     a.out = out;
     a.ws_o = (float*)((char*)workspace + 256);
     a.ws_ml = (float2*)((char*)workspace + 256 + sums);
-    a.ws_kn = a.far_tiles ? (float*)((char*)workspace + 256 + sums + align_up((size_t)a.ws_rows * a.S * sizeof(float2), 256)) : nullptr;
+    char* w = (char*)workspace + 256 + sums + align_up((size_t)a.ws_rows * a.S * sizeof(float2), 256);
+    a.ws_parts = (int32_t*)w;
+    w += align_up((size_t)a.ws_rows / a.block_rows * 4, 256);
+    a.ws_kn = a.far_tiles ? (float*)w : nullptr;
     const hipError_t e = kf::launch_attend(a, p->d, p->dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(KF_EDEVICE, "prompt attention launch: %s", hipGetErrorString(e));
     g_err[0] = 0;

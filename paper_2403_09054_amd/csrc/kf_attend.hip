@@ -78,7 +78,7 @@ constexpr float kAttendFar = 40.0f;  // 65536 keys that are left out weigh less 
 constexpr float kAttendSlack = 8.0f;
 
 template <typename T, int D, typename SHAPE, bool BIAS>
-__global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeof(T) > 256 || D * (int)sizeof(T) * SHAPE::NB > 640 ? 1 : 2)) attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeof(T) > 256 || (SHAPE::WR * SHAPE::WK == 4 && D * (int)sizeof(T) * SHAPE::NB > 640) ? 1 : 2)) attend_kernel(const AttendArgs a) {
     constexpr int WR = SHAPE::WR, WK = SHAPE::WK, SB = SHAPE::SB, NB = SHAPE::NB, W = WR * WK, US = NB / (WK * SB);
     constexpr int EB = sizeof(T), RB = D * EB, CH = RB / 16, NT = W * kWave, BK = NB * 32, AHEAD = WK * SB * 32;
     constexpr int PT = BK * CH / NT;             // 16-byte pieces of a tile that a thread brings
@@ -184,14 +184,21 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
                     break;
                 }
             }
-            t0 = __builtin_amdgcn_readfirstlane(from) * kFarTile / BK;
+            t0 = from * kFarTile / BK;
         }
     }
+    // a workgroup walks at most a.chunk keys; one that walks all of them finishes its rows, of others the records are joined
+    int parts = 1;
     if (a.S > 1) {
-        const int each = (t1 - t0 + a.S - 1) / a.S;
-        t0 = min(t0 + split * each, t1);
+        const int each = a.chunk / BK;
+        parts = max((t1 - t0 + each - 1) / each, 1);
+        if (split >= parts) return;
+        t0 += split * each;
         t1 = min(t0 + each, t1);
+        if (split == 0 && tid == 0) a.ws_parts[unit * (unsigned)a.tiles + (unsigned)qt] = parts;
     }
+    t0 = __builtin_amdgcn_readfirstlane(t0);     // (what the loads' bases are formed from)
+    t1 = __builtin_amdgcn_readfirstlane(t1);
     const int first = off + min(R0 + wr * 32, rows - 1) / a.G;  // of the wave
     const int last = R0 + wr * 32 < rows ? off + min(R0 + wr * 32 + 31, rows - 1) / a.G : -1;
     const int lowest = off + R0 / a.G;           // of the workgroup
@@ -433,7 +440,7 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
                 }
         }
     }
-    if (a.S > 1) {
+    if (parts > 1) {
         const int64_t row = ((int64_t)unit * a.tiles * ROWS + R) * a.S + split;
         if (half == 0) a.ws_ml[row] = make_float2(m, l);
         float* w = a.ws_o + row * D;
@@ -509,14 +516,16 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
     else if (a.seq_m) nk = a.seq_m[b];
     if (nq < 1 || nq > a.n || nk < 0 || nk > a.m || q0 < 0 || k0 < 0 || R >= nq * a.G) return;
     const int qi = R / a.G, qh = h * a.G + (R - qi * a.G);
+    const int parts = a.ws_parts[unit * a.tiles + R / a.block_rows];
+    if (parts == 1) return;
     const int64_t row = at * a.S;
     float m = -INFINITY;
-    for (int s = 0; s < a.S; ++s) m = fmaxf(m, a.ws_ml[row + s].x);
+    for (int s = 0; s < parts; ++s) m = fmaxf(m, a.ws_ml[row + s].x);
     const float ref = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    for (int s = 0; s < a.S; ++s) {
+    for (int s = 0; s < parts; ++s) {
         const float2 ml = a.ws_ml[row + s];
         const float by = hw_exp2(ml.x - ref);
         l = fmaf(by, ml.y, l);
@@ -532,35 +541,38 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
     }
 }
 
-// Shapes of a workgroup, by the bytes of a row: many rows; fewer; a few.
+// Shapes of a workgroup, by the bytes of a row: for many rows; for fewer; for about a workgroup of 64 rows a compute unit, whose waves are twice
+// as many; for a few rows.
 template <int RB>
 struct AttendShapes {
     using Many = AttendShape<4, 1, RB == 256 ? 2 : 1, 2>;
     using Fewer = AttendShape<2, 2, 1, 2>;
+    using One = AttendShape<2, 4, 1, 4>;
     using Few = AttendShape<1, 4, 1, 4>;
 };
 template <>
 struct AttendShapes<512> {
     using Many = AttendShape<4, 1, 1, 1>;
     using Fewer = AttendShape<2, 2, 1, 2>;
-    using Few = AttendShape<2, 2, 1, 2>;
 };
+enum { kAttendMany, kAttendFewer, kAttendOne, kAttendFew };
 
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
-    const int64_t units = (int64_t)a->B * a->H, rows = (int64_t)a->n * a->G;
+    const int64_t units = (int64_t)a->B * a->H, rows = (int64_t)a->n * a->G, b64 = units * ((rows + 63) / 64);
     const bool wide = d * (dtype == KF_F32 ? 4 : 2) > 256;
-    const int64_t slots = wide ? 256 : 512;      // workgroups that the chip holds at once
-    a->shape = units * ((rows + 127) / 128) >= 2 * slots ? 0 : units * ((rows + 63) / 64) >= slots / 2 || wide ? 1 : 2;
-    a->block_rows = a->shape == 0 ? 128 : a->shape == 1 || wide ? 64 : 32;
+    if (units * ((rows + 127) / 128) >= (wide ? 512 : 1024)) a->shape = kAttendMany;
+    else if (wide || b64 > 256) a->shape = kAttendFewer;
+    else a->shape = b64 > 64 ? kAttendOne : kAttendFew;
+    a->block_rows = a->shape == kAttendMany ? 128 : a->shape == kAttendFew ? 32 : 64;
     a->tiles = (int32_t)((rows + a->block_rows - 1) / a->block_rows);
     a->S = 1;
     const int64_t blocks = units * a->tiles;
-    const int64_t walk = ((int64_t)a->m + 127) / 128;
-    if (blocks < 256) {
-        int64_t S = 512 / blocks;
-        if (S > walk / 4) S = walk / 4;
-        if (S > 64) S = 64;
-        if (S > 1) a->S = (int32_t)S;
+    int64_t S = 256 / blocks;
+    if (S > a->m / 512) S = a->m / 512;
+    if (S > 64) S = 64;
+    if (S > 1) {
+        a->chunk = (int32_t)(((a->m + S - 1) / S + 127) / 128 * 128);
+        a->S = (a->m + a->chunk - 1) / a->chunk;
     }
     a->blocks = blocks * a->S;
     // A row of far tiles is looked for where a key is read often enough: the search reads K and V once more.
@@ -580,8 +592,10 @@ static hipError_t launch_attend_d(const AttendArgs& a, hipStream_t st) {
     using S = AttendShapes<D * (int)sizeof(T)>;
     if (a.far_tiles)
         hipLaunchKernelGGL((attend_norms_kernel<T, D>), dim3((unsigned)a.far_tiles, (unsigned)(a.B * a.H)), dim3(256), 0, st, a);
-    if (a.shape == 0) launch_attend_s<T, D, typename S::Many>(a, st);
-    else if (a.shape == 1) launch_attend_s<T, D, typename S::Fewer>(a, st);
+    if (a.shape == kAttendMany) launch_attend_s<T, D, typename S::Many>(a, st);
+    else if constexpr (D * sizeof(T) > 256) launch_attend_s<T, D, typename S::Fewer>(a, st);
+    else if (a.shape == kAttendFewer) launch_attend_s<T, D, typename S::Fewer>(a, st);
+    else if (a.shape == kAttendOne) launch_attend_s<T, D, typename S::One>(a, st);
     else launch_attend_s<T, D, typename S::Few>(a, st);
     if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * a.block_rows);
     return hipGetLastError();

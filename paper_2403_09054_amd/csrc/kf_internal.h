@@ -323,11 +323,13 @@ struct AttendArgs {
     float sc;                // |scale| * log2(e); the queries take the scale's sign, or zero with it
     uint32_t q_keep, q_flip;
     int32_t shape, block_rows;  // of a workgroup: many rows, fewer, a few
-    int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys
+    int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys at most
+    int32_t chunk;           // keys that each of them walks
     int32_t far_tiles;       // of a cached head, whose norms tell what a position bias rules out; 0: not looked for
     int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
     float* ws_o;             // [ws_rows][S][d]
     float2* ws_ml;           // [ws_rows][S] reference and sum
+    int32_t* ws_parts;       // [B*H][tiles] how many share a block's walk
     float* ws_kn;            // [B*H][far_tiles], or NULL
 };
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype);
