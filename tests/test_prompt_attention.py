@@ -208,6 +208,53 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, d, n, m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,H,G,n,m,packed", [(kf.BF16, 128, 2, 1, 2300, 2300, False), (kf.F16, 64, 1, 4, 700, 2100, False), (kf.F32, 64, 1, 2, 1100, 1100, True),
+                                                    (kf.BF16, 256, 1, 1, 2048, 2200, True)])
+def test_far_keys_are_left_out_only_where_they_cannot_matter(dtype, d, H, G, n, m, packed):
+    """Slopes from steep to none and rising ones, a far key that is long, far keys and values that are no numbers: as the definition has it."""
+    dt, HQ, g = TYPES[dtype], H * G, torch.Generator().manual_seed(n)
+    Q, K, V = (torch.randn((h, r, d), generator=g).to(dt) for h, r in ((HQ, n), (H, m), (H, m)))
+    scale = d ** -0.5
+    slopes = torch.tensor([0.9, 0.02, 0.3, 0.0][:HQ])
+    start = torch.tensor([0, n], dtype=torch.int32), torch.tensor([0, m], dtype=torch.int32)
+
+    def run(slopes):
+        out = torch.zeros((1, n, HQ, d), dtype=dt, device="cuda")
+        of = dict(B=1, n=n, m=m, H=H, q_per_kv=G, d=d, dtype=dtype, scale=scale, slopes=slopes.cuda())
+        if packed:
+            p = kf.Prompt(q_start=start[0].cuda(), k_start=start[1].cuda(), **of)
+            args = [x.transpose(0, 1).contiguous().cuda() for x in (Q, K, V)]
+        else:
+            p, args = kf.Prompt(**of), [x[None].cuda() for x in (Q, K, V)]
+        assert binding.lib().kf_prompt_workspace_bytes(p.c_struct()) > 256  # it is long enough to look for far keys
+        kf.kf_prompt_attend(p, *args, out, workspace=kf.new_prompt_workspace(p))
+        return out[0].transpose(0, 1)
+
+    def check(slopes, what):
+        want, tol = oracle(Q, K, V, scale, slopes, G, dt)
+        near(run(slopes), want, tol, what)
+
+    check(slopes, "slopes")
+    check(torch.full((HQ,), -0.004), "rising")
+    far = m // 50
+    keep = K[:, far].clone()
+    K[:, far] = Q[::G, n - 1] * 40.0  # a key that the last row asks for, far away
+    check(torch.full((HQ,), 0.1), "a long far key")
+    K[:, far] = keep
+    steep = torch.full((HQ,), 0.9)
+    clean = run(steep).double().cpu()
+    first = max(0, far - (m - n))
+    for tensor, value in ((V, math.inf), (V, math.nan), (K, math.nan)):
+        keep = tensor[0, far].clone()
+        tensor[0, far, 3] = value
+        got = run(steep).double().cpu()
+        assert bool(torch.isfinite(got[:G, :first]).all()) and torch.equal(got[G:], clean[G:])
+        bad = got[:G, first:, 3] if tensor is V else got[:G, first:]
+        assert not bool(torch.isfinite(bad).any())
+        tensor[0, far] = keep
+
+
+@pytest.mark.gpu
 def test_keys_at_minus_infinity_and_sequences_that_are_none():
     d, n = 64, 40
     Q = torch.ones((1, 1, n, d), dtype=torch.bfloat16, device="cuda")
