@@ -1002,7 +1002,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     a->q_keep = p->scale == 0.0f ? 0u : ~0u;
     a->q_flip = p->scale < 0.0f ? (eb == 2 ? 0x80008000u : 0x80000000u) : 0u;
     kf::plan_attend(a, p->d, p->dtype);
-    if (a->blocks > kMaxGrid - 8) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
+    if (a->blocks > kMaxGrid) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
     *sums = align_up((size_t)a->ws_rows * a->S * p->d * 4, 256);
     // records and their references, parts, far tiles
     *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256) + align_up((size_t)a->ws_rows / a->block_rows * 4, 256) +

@@ -96,25 +96,33 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
 
     // The workgroups of a cached head share an XCD and its L2.  Where the heads are a multiple of the XCDs each takes its share of every
     // sequence's, to and fro and another share for the next sequence, the last heads first: what a position bias leaves them to do grows
-    // with their number.  Else an XCD takes a run of neighbouring workgroups.
-    const unsigned per = (unsigned)(a.tiles * a.S), xcd = blockIdx.x % kXcds, place = blockIdx.x / kXcds;
-    unsigned rest;
+    // with their number.  Else a head's blocks of rows are dealt out to as many XCDs as it takes to give each the same number, and the
+    // heads of an XCD lie apart, so that no XCD has the long sequences or the heads with much to do.
+    const unsigned xcd = blockIdx.x % kXcds, place = blockIdx.x / kXcds, spread = (unsigned)a.spread;
+    const unsigned blocks = ((unsigned)a.tiles + spread - 1) / spread, per = blocks * (unsigned)a.S, local = place / per, rest = place - local * per;
+    unsigned block = rest / (unsigned)a.S;
+    int split = (int)(rest - block * (unsigned)a.S);
     int b, h;
     if (a.H % kXcds == 0) {
-        const unsigned local = place / per, back = local / (unsigned)a.B, r = (unsigned)a.H / kXcds - 1 - back;
-        rest = place - local * per;
+        const unsigned back = local / (unsigned)a.B, r = (unsigned)a.H / kXcds - 1 - back;
         b = (int)(local - back * (unsigned)a.B);
         const unsigned x = (xcd + (unsigned)b) % kXcds;
         h = (int)(r * kXcds + (r & 1 ? kXcds - 1 - x : x));
     } else {
-        const unsigned at = xcd * (gridDim.x / kXcds) + place;
-        if (at >= (unsigned)a.blocks) return;
-        rest = at % per;
-        b = (int)(at / per / (unsigned)a.H);
-        h = (int)(at / per - (unsigned)b * (unsigned)a.H);
+        const unsigned group = local * kXcds + xcd;
+        unsigned u = group / spread;
+        block = block * spread + group % spread;
+        if (spread == 1) {                       // heads of few blocks: one after the other
+            const unsigned at = blockIdx.x / (unsigned)a.S;
+            u = at / (unsigned)a.tiles;
+            block = at - u * (unsigned)a.tiles;
+            split = (int)(blockIdx.x - at * (unsigned)a.S);
+        } else if (block >= (unsigned)a.tiles) return;
+        b = (int)(u / (unsigned)a.H);
+        h = a.H - 1 - (int)(u - (unsigned)b * (unsigned)a.H);
     }
     const unsigned unit = (unsigned)b * (unsigned)a.H + (unsigned)h;
-    const int qt = a.tiles - 1 - (int)(rest / (unsigned)a.S), split = (int)(rest % (unsigned)a.S);  // long walks first
+    const int qt = a.tiles - 1 - (int)block;     // long walks first
 
     int64_t q0 = 0, k0 = 0;
     int nq = a.n, nk = a.m;
@@ -574,7 +582,10 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
         a->chunk = (int32_t)(((a->m + S - 1) / S + 127) / 128 * 128);
         a->S = (a->m + a->chunk - 1) / a->chunk;
     }
-    a->blocks = blocks * a->S;
+    a->spread = 1;
+    while (units * a->spread % kXcds) a->spread *= 2;
+    if (a->H % kXcds == 0 || a->tiles < 4 * a->spread) a->spread = 1;
+    a->blocks = units * a->spread * ((a->tiles + a->spread - 1) / a->spread) * a->S;  // of the launch
     // A row of far tiles is looked for where a key is read often enough: the search reads K and V once more.
     a->far_tiles = a->slopes && (int64_t)a->n * a->G >= 2048 && units <= 65535 ? (a->m + kFarTile - 1) / kFarTile : 0;
     a->ws_rows = a->S > 1 ? blocks * a->block_rows : 0;
@@ -582,8 +593,7 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
 
 template <typename T, int D, typename SHAPE>
 static void launch_attend_s(const AttendArgs& a, hipStream_t st) {
-    const int64_t run = (a.blocks + kXcds - 1) / kXcds;
-    const dim3 grid((unsigned)(run * kXcds)), block(SHAPE::WR * SHAPE::WK * kWave);
+    const dim3 grid((unsigned)a.blocks), block(SHAPE::WR * SHAPE::WK * kWave);
     if (a.slopes) hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, false>), grid, block, 0, st, a);
 }

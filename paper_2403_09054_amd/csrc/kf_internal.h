@@ -325,6 +325,7 @@ struct AttendArgs {
     int32_t shape, block_rows;  // of a workgroup: many rows, fewer, a few
     int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys at most
     int32_t chunk;           // keys that each of them walks
+    int32_t spread;          // XCDs that a cached head's blocks are dealt out to
     int32_t far_tiles;       // of a cached head, whose norms tell what a position bias rules out; 0: not looked for
     int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
     float* ws_o;             // [ws_rows][S][d]
