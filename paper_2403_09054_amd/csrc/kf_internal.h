@@ -363,6 +363,7 @@ struct PageArgs {
     int32_t L, B, H, G, pages, max_pages;
     int32_t n, rows, kept;   // new tokens at most, rows a head of k and v has room for, tokens that stay
     int32_t S, chunk;        // splits of a unit, pages of a split
+    int32_t waves;           // of a workgroup of the step
     float sc;                // scale * log2(e)
 };
 int32_t page_most_splits(int64_t U, int32_t max_pages);

@@ -19,8 +19,7 @@ namespace kf {
 
 constexpr int kPageThreads = 256;
 constexpr int kPageWaves = kPageThreads / kWave;
-constexpr int kStepWaves = 4;
-constexpr int kStepThreads = kStepWaves * kWave;
+constexpr int kStepWaves = 4;        // of a workgroup of the step; one where units have a page or two
 constexpr int kTableThreads = 1024;
 
 typedef __bf16 p_bf2_t __attribute__((ext_vector_type(2)));
@@ -679,11 +678,12 @@ __device__ __forceinline__ void page_append(const T* row, uint8_t* dst, float* s
 }
 
 // blockIdx.x = unit * S + split, unit = (layer * B + row) * H + head.  A split is a.chunk pages, shared out to the waves.
-template <typename T, int D, bool BIAS>
-__global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs a) {
+template <typename T, int D, bool BIAS, int NW>
+__global__ void __launch_bounds__(NW * kWave, 2) page_step_kernel(const PageArgs a) {
     constexpr int C = D / 64, NQ = D / 32, DT = D / 16;
-    __shared__ float o_s[kStepWaves][8][D];
-    __shared__ float m_s[kStepWaves][8], l_s[kStepWaves][8];
+    constexpr int PARTS = D > 128 ? 2 : 1, CP = C / PARTS, DP = DT / PARTS;  // a page of wide rows is held by halves: two waves on a SIMD
+    __shared__ float o_s[NW][8][D];
+    __shared__ float m_s[NW][8], l_s[NW][8];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n0 = lane & 15, g = lane >> 4;
     const unsigned u = blockIdx.x / (unsigned)a.S;
     const int split = (int)(blockIdx.x - u * (unsigned)a.S);
@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
     float* out = a.out + (int64_t)u * a.G * D;
     if (!asked || !there) {
         if (split == 0) {
-            for (int i = tid; i < a.G * D; i += kStepThreads) out[i] = 0.0f;
+            for (int i = tid; i < a.G * D; i += NW * kWave) out[i] = 0.0f;
             if (asked && tid == 0) count_error(a);
         }
         return;
@@ -707,10 +707,11 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
     if (split > owner) return;
     const int p1 = split == owner ? tail + ((old & 63) != 0) : p0 + a.chunk;
 
-    // A page's keys are asked for when the last one's are used up, its values likewise: a wave has half a page or a page under way always.
-    uint4 k[4][C], v[DT];
+    // A page's keys (or the half of them) are asked for when those before are used up, its values likewise: a wave always has some under way.
+    uint4 k[4][CP], v[DP];
     float ks = 0.0f, vs = 0.0f;
     int page = -1;
+    int64_t at = 0;
     const uint32_t klane = ((n0 >> 2) * 16 + (n0 & 3)) * D + g * 16, vlane = n0 * 64 + g * 16;
     auto find = [&](int j) {                     // a number that is no page's leaves the page's tokens out, and page 0 is read
         page = ahead;
@@ -718,28 +719,27 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
             if (lane == 0) count_error(a);
             page = -1;
         }
-        ahead = uniform_load(table + min(j + kStepWaves, a.max_pages - 1));
+        ahead = uniform_load(table + min(j + NW, a.max_pages - 1));
+        return ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
     };
-    auto bring_keys = [&]() {
-        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
-        const uint8_t* kp = a.K + at * 64 * D + klane;
+    auto bring_keys = [&](int64_t tile, int part) {
+        const uint8_t* kp = a.K + tile * 64 * D + part * CP * 64 + klane;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int c = 0; c < C; ++c) k[t][c] = stream_load((const uint4*)(kp + t * 4 * D + c * 64));
-        ks = uniform_load(a.k_scale + at) * a.sc;
+            for (int c = 0; c < CP; ++c) k[t][c] = stream_load((const uint4*)(kp + t * 4 * D + c * 64));
+        if (part == 0) ks = uniform_load(a.k_scale + tile) * a.sc;
     };
-    auto bring_values = [&]() {
-        const int64_t at = ((int64_t)l * a.pages + max(page, 0)) * a.H + h;
-        const uint8_t* vp = a.V + at * 64 * D + vlane;
+    auto bring_values = [&](int64_t tile, int part) {
+        const uint8_t* vp = a.V + tile * 64 * D + part * DP * 16 * 64 + vlane;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) v[i] = stream_load((const uint4*)(vp + i * 16 * 64));
-        vs = uniform_load(a.v_scale + at);
+        for (int i = 0; i < DP; ++i) v[i] = stream_load((const uint4*)(vp + i * 16 * 64));
+        if (part == 0) vs = uniform_load(a.v_scale + tile);
     };
-    find(p0 + wv);
     if (p0 + wv < p1) {
-        bring_keys();
-        bring_values();
+        at = find(p0 + wv);
+        bring_keys(at, 0);
+        bring_values(at, 0);
     }
 
     const int head = n0 & 7, part = n0 >> 3;     // of this lane's column
@@ -778,21 +778,29 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
         }
     }
 
-    for (int j = p0 + wv; j < p1; j += kStepWaves) {
+    for (int j = p0 + wv; j < p1; j += NW) {
         const int live = page < 0 ? 0 : old;     // tokens that are there
         const float kby = ks, vby = vs;
+        const bool more = j + NW < p1;
+        int64_t next = at;
         p_f4_t x[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            x[t] = p_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < 4; ++t) x[t] = p_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                x[t] = code_product<T>(k[t][c].x, k[t][c].y, q[2 * c], x[t]);
-                x[t] = code_product<T>(k[t][c].z, k[t][c].w, q[2 * c + 1], x[t]);
+        for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < CP; ++c) {
+                    x[t] = code_product<T>(k[t][c].x, k[t][c].y, q[2 * (part * CP + c)], x[t]);
+                    x[t] = code_product<T>(k[t][c].z, k[t][c].w, q[2 * (part * CP + c) + 1], x[t]);
+                }
+            if (part + 1 < PARTS) bring_keys(at, part + 1);
+            else if (more) {
+                next = find(j + NW);
+                bring_keys(next, 0);
             }
         }
-        find(j + kStepWaves);
-        if (j + kStepWaves < p1) bring_keys();
         const int j0 = j * 64 + g * 16;          // token of x[t][r]: j0 + 4 t + r
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -801,6 +809,7 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
                 if constexpr (BIAS) x[t][r] = fmaf(x[t][r], kby, slope * (float)(j0 + 4 * t + r - old));
                 else x[t][r] *= kby;
             }
+        uint4 tail_mask = make_uint4(~0u, ~0u, ~0u, ~0u);
         if (j * 64 + 64 > live) {                // the last page: slots that hold no token of this sequence, or the new one's
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -810,8 +819,7 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
             uint32_t mask[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) mask[i] = have - 4 * i >= 4 ? ~0u : have - 4 * i <= 0 ? 0u : (1u << 8 * (have - 4 * i)) - 1u;
-#pragma unroll
-            for (int i = 0; i < DT; ++i) v[i].x &= mask[0], v[i].y &= mask[1], v[i].z &= mask[2], v[i].w &= mask[3];
+            tail_mask = make_uint4(mask[0], mask[1], mask[2], mask[3]);
         }
         float top = x[0][0];
 #pragma unroll
@@ -840,14 +848,23 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
                 p[t >> 1][(t & 1) * 4 + r + 1] = w.y;
             }
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            p_f4_t y = p_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].x, v[i].y), p[0], y, 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].z, v[i].w), p[1], y, 0, 0, 0);
+        for (int part = 0; part < PARTS; ++part) {
+            if (j * 64 + 64 > live) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[i][r] = fmaf(y[r], vby, o[i][r]);
+                for (int i = 0; i < DP; ++i) v[i].x &= tail_mask.x, v[i].y &= tail_mask.y, v[i].z &= tail_mask.z, v[i].w &= tail_mask.w;
+            }
+#pragma unroll
+            for (int i = 0; i < DP; ++i) {
+                p_f4_t y = p_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].x, v[i].y), p[0], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves8(v[i].z, v[i].w), p[1], y, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[part * DP + i][r] = fmaf(y[r], vby, o[part * DP + i][r]);
+            }
+            if (part + 1 < PARTS) bring_values(at, part + 1);
+            else if (more) bring_values(next, 0);
         }
-        if (j + kStepWaves < p1) bring_values();
+        at = next;
     }
 
     sum = across_sum(sum);
@@ -860,15 +877,15 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
         }
     if (lane < 8) m_s[wv][lane] = m, l_s[wv][lane] = sum;
     __syncthreads();
-    for (int i = tid; i < a.G * D; i += kStepThreads) {
+    for (int i = tid; i < a.G * D; i += NW * kWave) {
         const int y = i / D, d = i - y * D;
         float top = m_s[0][y];
 #pragma unroll
-        for (int w = 1; w < kStepWaves; ++w) top = fmaxf(top, m_s[w][y]);
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, m_s[w][y]);
         const float ref = top == -INFINITY ? 0.0f : top;
         float s = 0.0f, v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kStepWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float by = hw_exp2(m_s[w][y] - ref);
             s = fmaf(by, l_s[w][y], s);
             v = fmaf(by, o_s[w][y][d], v);
@@ -881,10 +898,11 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(const PageArgs 
         }
     }
     if (split == owner && wv < 2) {              // every wave is done with the page
-        const int page = uniform_load(table + tail);
-        if ((unsigned)page < (unsigned)a.pages) {
-            const int64_t at = ((int64_t)l * a.pages + page) * a.H + h;
-            page_append<T, D>(wv ? vn : kn, (wv ? a.V : a.K) + at * 64 * D, (wv ? a.v_scale : a.k_scale) + at, old & 63, wv != 0, lane);
+        const int last = uniform_load(table + tail);
+        if ((unsigned)last < (unsigned)a.pages) {
+            const int64_t to = ((int64_t)l * a.pages + last) * a.H + h;
+            for (int tensor = wv; tensor < 2; tensor += NW)
+                page_append<T, D>(tensor ? vn : kn, (tensor ? a.V : a.K) + to * 64 * D, (tensor ? a.v_scale : a.k_scale) + to, old & 63, tensor != 0, lane);
         } else if (tid == 0 && (old & 63) == 0) count_error(a);
     }
 }
@@ -941,13 +959,19 @@ void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint) {
     const int32_t S = page_most_splits(U, pages);
     a->chunk = (pages + S - 1) / S;
     a->S = (pages + a->chunk - 1) / a->chunk;
+    a->waves = a->S == 1 && (pages == 1 || (pages == 2 && U >= 512)) ? 1 : kStepWaves;
 }
 
 template <typename T, int D>
 static void launch_step_d(const PageArgs& a, int64_t U, hipStream_t st) {
-    const dim3 grid((unsigned)(U * a.S)), block(kStepThreads);
-    if (a.slopes) hipLaunchKernelGGL((page_step_kernel<T, D, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((page_step_kernel<T, D, false>), grid, block, 0, st, a);
+    const dim3 grid((unsigned)(U * a.S));
+    if (a.waves == 1) {
+        if (a.slopes) hipLaunchKernelGGL((page_step_kernel<T, D, true, 1>), grid, dim3(kWave), 0, st, a);
+        else hipLaunchKernelGGL((page_step_kernel<T, D, false, 1>), grid, dim3(kWave), 0, st, a);
+    } else {
+        if (a.slopes) hipLaunchKernelGGL((page_step_kernel<T, D, true, kStepWaves>), grid, dim3(kStepWaves * kWave), 0, st, a);
+        else hipLaunchKernelGGL((page_step_kernel<T, D, false, kStepWaves>), grid, dim3(kStepWaves * kWave), 0, st, a);
+    }
     if (a.S > 1) hipLaunchKernelGGL((page_join_kernel<D>), dim3((unsigned)(U * a.G)), dim3(kPageThreads), 0, st, a);
 }
 template <typename T, int D>
