@@ -499,8 +499,11 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
 // values are turned in LDS.
 template <typename T, int D>
 __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs a) {
-    constexpr int CH = D / 8, PT = 64 * CH / kPageThreads, PITCH = 64 + 16;
+    constexpr int CH = D / 8, PT = 64 * CH / kPageThreads, Y = PT < 4 ? PT : 4, PITCH = 64 + 4;
     __shared__ __attribute__((aligned(16))) uint8_t turn[D * PITCH];
+    // piece x of a thread: Y neighbouring tokens, then the next group of them
+    auto token_of = [](int x) { return ((int)threadIdx.x / CH + x / Y * (kPageThreads / CH)) * Y + x % Y; };
+    const int column = (int)threadIdx.x % CH;
     __shared__ float red[kPageWaves];
     const int tid = threadIdx.x;
     const unsigned pages = (unsigned)(a.n + 62) / 64 + 1, rest = blockIdx.x / (unsigned)a.H;
@@ -522,14 +525,26 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
     const int s0 = max(first - j * 64, 0), s1 = min(len - j * 64, 64);  // slots of the new rows
     const int64_t at = ((int64_t)l * a.pages + page) * a.H + h;
     uint4 rows[2][PT];
+    // what the page holds already, where not all of it is new: in the same trip
+    constexpr int OT = 64 * D / 16 / kPageThreads;
+    const bool beside = s0 > 0 || s1 < 64;
+    uint4 held[2][OT];
+    int was[2];
 #pragma unroll
     for (int tensor = 0; tensor < 2; ++tensor) {
+        const uint4* dst = (const uint4*)((tensor ? a.V : a.K) + at * 64 * D);
+        was[tensor] = exponent_of(uniform_load((tensor ? a.v_scale : a.k_scale) + at));
+#pragma unroll
+        for (int x = 0; x < OT; ++x) {
+            held[tensor][x] = make_uint4(0u, 0u, 0u, 0u);
+            if (beside) held[tensor][x] = dst[tid + x * kPageThreads];
+        }
         const T* src = (const T*)(tensor ? a.v : a.k) + (((int64_t)lb * a.H + h) * a.rows + (j * 64 - first)) * D;  // row of slot 0
 #pragma unroll
         for (int x = 0; x < PT; ++x) {
-            const int p = tid + x * kPageThreads, t = p / CH;
+            const int t = token_of(x);
             rows[tensor][x] = make_uint4(0u, 0u, 0u, 0u);
-            if (t >= s0 && t < s1) rows[tensor][x] = stream_load((const uint4*)(src + t * D) + p % CH);
+            if (t >= s0 && t < s1) rows[tensor][x] = stream_load((const uint4*)(src + t * D) + column);
         }
     }
 #pragma unroll
@@ -548,39 +563,64 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
         int e = page_exponent(block_most(most, red));
         float ratio = 1.0f;                      // of the older rows' scale to the new one
         if (s0 > 0) {
-            const int old = exponent_of(*scale);
-            e = max(e, old);
-            ratio = power_of_two(max(old - e, -126));
+            e = max(e, was[tensor]);
+            ratio = power_of_two(max(was[tensor] - e, -126));
         }
         const float inv = power_of_two(-e);
         if (tensor == 0) {
 #pragma unroll
             for (int x = 0; x < PT; ++x) {
-                const int p = tid + x * kPageThreads, t = p / CH;
+                const int t = token_of(x);
                 float f[8];
                 unpack16<T>(r[x], f);
-                if (t >= s0 && t < s1) *(uint2*)(dst + p * 8) = make_uint2(encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv));
+                if (t >= s0 && t < s1) *(uint2*)(dst + t * D + column * 8) = make_uint2(encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv));
             }
-            if (ratio != 1.0f)
-                for (int p = tid; p < s0 * (D / 4); p += kPageThreads) ((uint32_t*)dst)[p] = again4(((uint32_t*)dst)[p], ratio);
+            if (ratio != 1.0f) {
+#pragma unroll
+                for (int x = 0; x < OT; ++x) {
+                    const int p = tid + x * kPageThreads;
+                    const uint4 o = held[0][x];
+                    if (p < s0 * (D / 16)) ((uint4*)dst)[p] = make_uint4(again4(o.x, ratio), again4(o.y, ratio), again4(o.z, ratio), again4(o.w, ratio));
+                }
+            }
         } else {
+            // an element of Y tokens is one write to LDS (a byte at a time, 16 lanes on a bank, 512-byte rows took twice as long)
 #pragma unroll
-            for (int x = 0; x < PT; ++x) {
-                const int p = tid + x * kPageThreads, t = p / CH, c = p % CH * 8;
-                float f[8];
-                unpack16<T>(r[x], f);
-                const uint32_t w[2] = {encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv)};
+            for (int x = 0; x < PT; x += Y) {
+                uint32_t w[Y][2];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) turn[(c + i) * PITCH + t] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+                for (int y = 0; y < Y; ++y) {
+                    float f[8];
+                    unpack16<T>(r[x + y], f);
+                    w[y][0] = encode4(f[0], f[1], f[2], f[3], inv), w[y][1] = encode4(f[4], f[5], f[6], f[7], inv);
+                }
+                uint8_t* to = turn + column * 8 * PITCH + token_of(x);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    if constexpr (Y == 4) {
+                        const uint32_t a01 = __builtin_amdgcn_perm(w[1][q], w[0][q], 0x05010400u), b01 = __builtin_amdgcn_perm(w[1][q], w[0][q], 0x07030602u);
+                        const uint32_t a23 = __builtin_amdgcn_perm(w[3][q], w[2][q], 0x05010400u), b23 = __builtin_amdgcn_perm(w[3][q], w[2][q], 0x07030602u);
+                        *(uint32_t*)(to + (4 * q) * PITCH) = __builtin_amdgcn_perm(a23, a01, 0x05040100u);
+                        *(uint32_t*)(to + (4 * q + 1) * PITCH) = __builtin_amdgcn_perm(a23, a01, 0x07060302u);
+                        *(uint32_t*)(to + (4 * q + 2) * PITCH) = __builtin_amdgcn_perm(b23, b01, 0x05040100u);
+                        *(uint32_t*)(to + (4 * q + 3) * PITCH) = __builtin_amdgcn_perm(b23, b01, 0x07060302u);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *(uint16_t*)(to + (4 * q + i) * PITCH) = (uint16_t)((w[0][q] >> (8 * i) & 255u) | (w[Y - 1][q] >> (8 * i) & 255u) << 8);
+                    }
+                }
             }
             __syncthreads();
-            for (int p = tid; p < D * 4; p += kPageThreads) {
-                const int d = p >> 2, t = (p & 3) * 16;
+#pragma unroll
+            for (int x = 0; x < OT; ++x) {
+                const int p = tid + x * kPageThreads, d = p >> 2, t = (p & 3) * 16;
                 if (t + 16 <= s0 && ratio == 1.0f) continue;
                 if (t >= s1) continue;
-                uint4 v = *(const uint4*)(turn + d * PITCH + t);
+                const uint32_t* from = (const uint32_t*)(turn + d * PITCH + t);
+                uint4 v = make_uint4(from[0], from[1], from[2], from[3]);
                 if (t < s0 || t + 16 > s1) {     // older rows or none beside them
-                    const uint4 o = *(const uint4*)(dst + d * 64 + t);
+                    const uint4 o = held[1][x];
                     uint32_t w[4] = {v.x, v.y, v.z, v.w};
                     const uint32_t had[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
@@ -599,8 +639,7 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
                 *(uint4*)(dst + d * 64 + t) = v;
             }
         }
-        __syncthreads();                         // the scale was read
-        if (tid == 0) *scale = power_of_two(e);
+        if (tid == 0) *scale = power_of_two(e);  // (read by the whole workgroup ahead of a barrier)
     }
 }
 
