@@ -222,15 +222,15 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     uint32_t koff[NV], voff[NV];
 #pragma unroll
     for (int x = 0; x < NV; ++x) {
-        const int row = tid / CH, c = tid % CH;
-        koff[x] = (uint32_t)row * (uint32_t)krow + key_piece(row + x * RPX, c) * 16;
-        voff[x] = (uint32_t)row * (uint32_t)vrow + value_piece(row + x * RPX, c) * 16;
+        const int row = tid / CH, mine = lane / CH, c = tid % CH;
+        koff[x] = (uint32_t)mine * (uint32_t)krow + key_piece(row + x * RPX, c) * 16;
+        voff[x] = (uint32_t)mine * (uint32_t)vrow + value_piece(row + x * RPX, c) * 16;
     }
     const uint32_t klds = (uint32_t)(uintptr_t)(lds_char*)kbuf + wv * 1024, vlds = (uint32_t)(uintptr_t)(lds_char*)vbuf + wv * 1024;
     // rows [r0, r0 + BK) of K or V; what lies outside the sequence is its nearest row again
     auto bring_rows = [&](int r0, const char* base, int64_t pitch, uint32_t lds, const uint32_t (&off)[NV], auto piece) {
         if (r0 >= 0 && r0 + BK <= nk) {
-            const char* p = base + (int64_t)r0 * pitch;
+            const char* p = base + (int64_t)(r0 + wv * (kWave / CH)) * pitch;
 #pragma unroll
             for (int x = 0; x < PT; ++x) to_lds(lds + x * NT * 16, p + x * RPX * pitch, off[x % NV]);
         } else {

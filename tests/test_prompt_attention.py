@@ -308,6 +308,23 @@ def test_far_rows_pass_32_bits():
 
 
 @pytest.mark.gpu
+def test_far_rows_pass_32_bits_inside_a_tile():
+    """Tiles of 128 keys whose tokens lie 2^27 bytes apart, shared by workgroups of eight waves."""
+    H, n, m, d, step = 40, 128, 130, 64, 1 << 26
+    flat = torch.empty(step * (m - 1) + 2 * H * d, dtype=torch.bfloat16, device="cuda")
+    K, V = (torch.as_strided(flat, (1, H, m, d), (0, d, step, 1), i * H * d) for i in range(2))
+    g = torch.Generator().manual_seed(2)
+    for x in (K, V):
+        x.copy_(torch.randn((1, H, m, d), generator=g).bfloat16())
+    Q = torch.randn((1, H, n, d), generator=g).bfloat16().cuda()
+    out = torch.zeros((1, n, H, d), dtype=torch.bfloat16, device="cuda")
+    p = kf.Prompt(1, n, m, H, d, kf.BF16, 0.1, k_stride=(0, d, step), v_stride=(0, d, step))
+    kf.kf_prompt_attend(p, Q, K, V, out, workspace=kf.new_prompt_workspace(p))
+    want, tol = oracle(Q[0].cpu(), K[0].cpu(), V[0].cpu(), 0.1, None, 1, torch.bfloat16)
+    near(out[0].transpose(0, 1), want, tol, "far")
+
+
+@pytest.mark.gpu
 def test_replayed_graph_and_another_stream():
     for case in ((2, 130, 130, 2, 2, 128, kf.BF16, False, "plain"), (1, 2, 2000, 2, 1, 128, kf.BF16, False, "plain")):
         p, (Q, K, V, out), views, _, dt = make(case)
