@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     if constexpr (BIAS) {
         // Far keys that cannot matter.  A row's largest logit is at least its own key's; one at distance D is at most sc |q| |k| - slope D:
         // where that lies kAttendFar below for every row, a tile of keys is left out, with all before it.  (A tile that holds a value which
-        // is no number, or infinite, has an infinite norm; what is no number makes no row's bound hold.)
+        // is no number, or infinite, has an infinite norm; what is no number makes no row's bound hold, nor does a bias that rises.)
         if (a.ws_kn && t1 > 0) {
             float qq = 0.0f, own = 0.0f;
             const char* mine = Kh + (int64_t)min(max(pos, 0), nk - 1) * krow + half * 16;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
             }
             qq = half_sum(qq);
             own = half_sum(own);
-            const bool odd = __any(!(qq < INFINITY) || !(fabsf(own) < INFINITY));
+            const bool odd = __any(!(qq < INFINITY) || !(fabsf(own) < INFINITY) || slope < 0.0f);
             qq = odd ? INFINITY : wave_max(qq);
             own = wave_max(-own);
             const float flat = -wave_max(-slope);

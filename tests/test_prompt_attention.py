@@ -255,6 +255,21 @@ def test_far_keys_are_left_out_only_where_they_cannot_matter(dtype, d, H, G, n, 
 
 
 @pytest.mark.gpu
+def test_far_keys_that_a_rising_bias_prefers():
+    """The far end of a far tile has more of a negative slope than its near end: every row's first key outweighs its own."""
+    n, d, slope, g = 2304, 128, -10.0, torch.Generator().manual_seed(3)
+    row = torch.arange(n)
+    Q = torch.nn.functional.one_hot(row % d, d).bfloat16()[None]
+    K = torch.where(row >= n - d, -slope * row - 800.0, 0.0)[:, None].bfloat16() * Q
+    V = torch.randn((1, n, d), generator=g).bfloat16()
+    out = torch.zeros((1, n, 1, d), dtype=torch.bfloat16, device="cuda")
+    p = kf.Prompt(1, n, n, 1, d, kf.BF16, 1.0, slopes=torch.tensor([slope]).cuda())
+    kf.kf_prompt_attend(p, Q[None].cuda(), K[None].cuda(), V[None].cuda(), out, workspace=kf.new_prompt_workspace(p))
+    want, tol = oracle(Q, K, V, 1.0, torch.tensor([slope]), 1, torch.bfloat16)
+    near(out[0].transpose(0, 1), want, tol, "rising")
+
+
+@pytest.mark.gpu
 def test_keys_at_minus_infinity_and_sequences_that_are_none():
     d, n = 64, 40
     Q = torch.ones((1, 1, n, d), dtype=torch.bfloat16, device="cuda")
