@@ -74,8 +74,12 @@ __device__ __forceinline__ float half_sum(float v) {
 
 constexpr int kFarTile = 128;        // keys whose largest norm is kept
 constexpr float kAttendFar = 40.0f;  // 65536 keys that are left out weigh less than 2^-24 of a row together
-// A reference is raised once a row's largest exponent is this far above it; terms stay below 2^8.
+// A reference is raised once a row's largest exponent is this far above the place where raising puts it.
 constexpr float kAttendSlack = 8.0f;
+// Raising puts a row's reference this far below its largest exponent.  In half precision terms then reach from 2^15 down to 2^-24, so that
+// those below 2^-31 of the largest are all that is lost; the other types have bits of exponent enough.
+template <typename T>
+constexpr float kAttendLift = __is_same(T, f16_t) ? 7.0f : 0.0f;
 
 template <typename T, int D, typename SHAPE, bool BIAS>
 __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeof(T) > 256 || (SHAPE::WR * SHAPE::WK == 4 && D * (int)sizeof(T) * SHAPE::NB > 640) ? 1 : 2)) attend_kernel(const AttendArgs a) {
@@ -286,9 +290,9 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
         for (int c = 0; c < SB; ++c)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, x[c][r]);
-        return half_max(top) * sc;
+        return fmaf(half_max(top), sc, -kAttendLift<T>);
     };
-    // the reference, where the largest exponent asks for it
+    // the reference, where the largest exponent (less the lift) asks for it
     auto raise = [&](float top) {
         if (__any(top > m + kAttendSlack || m == -INFINITY)) {
             const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : hw_exp2(m - to);

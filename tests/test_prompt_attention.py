@@ -270,6 +270,23 @@ def test_far_keys_that_a_rising_bias_prefers():
 
 
 @pytest.mark.gpu
+def test_many_light_keys_beside_a_heavy_one():
+    """65535 keys of weight 2^-25.5 beside one of weight 1 have 1/700 of a row, in half precision too."""
+    H, n, m, d, dt = 64, 256, 65536, 64, torch.float16
+    K, V = torch.zeros((1, 1, m, d), dtype=dt), torch.ones((1, 1, m, d), dtype=dt)
+    K[0, 0, 7, 0], V[0, 0, 7] = 17.6875, 0.0
+    Q = torch.zeros((1, H, n, d), dtype=dt)
+    Q[..., 0] = 1.0
+    out = torch.zeros((1, n, H, d), dtype=dt, device="cuda")
+    p = kf.Prompt(1, n, m, H, d, kf.F16, 1.0, k_stride=(0, 0, d), v_stride=(0, 0, d))
+    kf.kf_prompt_attend(p, Q.cuda(), K.cuda(), V.cuda(), out, workspace=kf.new_prompt_workspace(p))
+    light = (m - n + torch.arange(n)).double() * math.exp(-17.6875)
+    want = (light / (1 + light))[:, None, None].expand(n, H, d)
+    # a term's 2^-21 and 2^-12, the sums' (m + 64) U, and the row's rounding: 2^-12 (halves as small as 2^-10 are normal)
+    near(out[0], want, want * (2.0 ** -21 + 2.0 ** -11 + (m + 64) * U), "light")
+
+
+@pytest.mark.gpu
 def test_keys_at_minus_infinity_and_sequences_that_are_none():
     d, n = 64, 40
     Q = torch.ones((1, 1, n, d), dtype=torch.bfloat16, device="cuda")
