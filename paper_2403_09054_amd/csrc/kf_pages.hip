@@ -819,7 +819,7 @@ __global__ void __launch_bounds__(NW * kWave, 2) page_step_kernel(const PageArgs
 
     for (int j = p0 + wv; j < p1; j += NW) {
         const int live = page < 0 ? 0 : old;     // tokens that are there
-        const float kby = ks, vby = vs;
+        const float kby = ks, vby = page < 0 ? 0.0f : vs;
         const bool more = j + NW < p1;
         int64_t next = at;
         p_f4_t x[4];
@@ -981,7 +981,8 @@ __global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs 
         v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    ((float4*)(a.out + ((int64_t)u * a.G + y) * D))[e] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    float* out = a.out + ((int64_t)u * a.G + y) * D + 4 * e;  // (of any alignment)
+    out[0] = v.x * inv, out[1] = v.y * inv, out[2] = v.z * inv, out[3] = v.w * inv;
 }
 
 // ---------------------------------------------------------------- launches

@@ -401,6 +401,28 @@ def test_tables_that_are_none_and_rows_without_room():
 
 
 # ---------------------------------------------------------------- a token's step
+@pytest.mark.gpu
+def test_a_page_number_that_is_none_beside_a_scale_that_is_no_number():
+    """The tokens of a page that there is not are left out; what page 0 holds does not come in their place."""
+    c, ws, m = both(1, 1, 1, 64, 4, 3)
+    g = torch.Generator().manual_seed(9)
+    fill(c, ws, m, g, [150])
+    c.table[0] = torch.tensor([1, 77, 2])
+    for x in (c.K, c.V):
+        x[:, 1:3] = x[:, [0, 2]].clone()
+        x[:, 0] = 0x7F
+    for x in (c.k_scale, c.v_scale):
+        x[:, 1:3] = x[:, [0, 2]].clone()
+        x[:, 0] = math.nan
+    q, k, v = (torch.randn((1, 1, 1, 64), generator=g).bfloat16() for _ in range(3))
+    out = torch.zeros((1, 1, 1, 64), device="cuda")
+    kf.kf_page_step(c, q.cuda(), k.cuda(), v.cuda(), 0.125, out, workspace=ws)
+    K, V = m.held(0, 0, 0)
+    at = [j for j in range(149) if j // P != 1]
+    want, tol = step_oracle(K[at], V[at], *(x[0, 0, 0].double().numpy() for x in (q, k, v)), 0.125, 0.0)
+    assert (np.abs(out[0, 0, 0].double().cpu().numpy() - want) <= tol).all()
+
+
 def step_oracle(K, V, q, kn, vn, scale, slope):
     """One head: held rows [m, d], the token's own -> its output and how far it may be off: d U of a logit's magnitudes and 6 U of its own size, 2^-21 of
     the exponential, 2^-20 for the two halves of 11 bits that a probability is held in (2^-34 of the largest where they become subnormal), the sums."""
