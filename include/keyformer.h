@@ -440,7 +440,8 @@ kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *sco
  * n and m bound a sequence's rows and keys; one whose rows lie outside [1, n] or whose keys lie outside [0, m] is left out.
  * Any q_per_kv is served.  out must not overlap the inputs.  The workspace (kf_prompt_workspace_bytes) needs no initial contents.
  * Errors: KF_EINVAL for sizes, null pointers, scale not finite, alignment (pointers and strides: 16 bytes), seq_n with q_start, seq_m
- * with k_start; KF_EUNSUPPORTED for a dtype / d pair that is not built; KF_EWORKSPACE.
+ * with k_start; KF_EUNSUPPORTED for a dtype / d pair that is not built, and for slopes beside a scale below 2^-60 in magnitude that is
+ * not zero; KF_EWORKSPACE.
  */
 typedef struct {
     int32_t B, n, m, H, q_per_kv, d, dtype; /* q_per_kv 0 means 1 */
@@ -467,7 +468,8 @@ kf_status kf_prompt_attend(const kf_prompt *p, const void *Q, const void *K, con
  *   table   : DEVICE [B][max_pages] page numbers of a sequence's tokens, in order; -1 behind them.  All -1 at first.
  *   len     : DEVICE [B] tokens of each sequence.  Zero at first.
  *   refs    : DEVICE [pages] sequences that hold a page; 0: free.  Zero at first.
- * Sequences share full pages only; a last page that is not full is its sequence's alone, so that no row is written to a shared page.
+ * Sequences share full pages only; a last page that is not full is its sequence's alone, so that no row is written to a shared page (a
+ * page that refs says several hold is left as it is, and the unit counted).
  * Pages are taken lowest number first, sequences in order.  table, len and refs serve all layers; a caller that runs its layers one
  * after the other passes the struct with L = 1 and the layer's K, V and scales to kf_page_write and kf_page_step.
  * dtype (KF_BF16 or KF_F16) is that of the rows that go in and of the queries.  d: 64, 128 or 256; q_per_kv: 1, 2, 4 or 8; B up to 8192.
@@ -486,7 +488,8 @@ size_t kf_page_workspace_bytes(const kf_pages *p);
 /* Room for n more tokens of every sequence, or seq_n[b] of them (DEVICE [B] or NULL; one outside [1, n] leaves its sequence as it
  * is): len grows by them, and pages are taken as they need.  A sequence for which the table or the free pages do not suffice is
  * left as it is and counted; the ones behind it may still find room.  The rows themselves are then written by kf_page_write or
- * kf_page_step, layer by layer. */
+ * kf_page_step, layer by layer.  These go by len alone: rows for a sequence that was left as it is would take the place of its last
+ * ones, so that a caller who may run out of pages looks at the count (or at len) first, or gives seq_n without that sequence. */
 kf_status kf_page_reserve(const kf_pages *p, int32_t n, const int32_t *seq_n, void *workspace, size_t workspace_bytes, void *stream);
 
 /* The rows of the last n (or seq_n[b]) tokens of every sequence, as just reserved: k and v are DEVICE [L][B][H][rows][d], rows [0, n)

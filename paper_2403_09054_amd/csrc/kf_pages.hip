@@ -528,6 +528,7 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
     // what the page holds already, where not all of it is new: in the same trip
     constexpr int OT = 64 * D / 16 / kPageThreads;
     const bool beside = s0 > 0 || s1 < 64;
+    const int holders = uniform_load(a.refs + page);
     uint4 held[2][OT];
     int was[2];
 #pragma unroll
@@ -546,6 +547,10 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
             rows[tensor][x] = make_uint4(0u, 0u, 0u, 0u);
             if (t >= s0 && t < s1) rows[tensor][x] = stream_load((const uint4*)(src + t * D) + column);
         }
+    }
+    if (holders > 1) {                           // others hold the page: no room was reserved
+        if (tid == 0) count_error(a);
+        return;
     }
 #pragma unroll
     for (int tensor = 0; tensor < 2; ++tensor) {
@@ -679,10 +684,11 @@ __device__ __forceinline__ float across_sum(float v) {
 constexpr float kPageLift = 10.0f;   // probabilities are held 2^10 times as large, so that their lower half stays a normal number
 constexpr float kPageSlack = 4.0f;   // a reference is raised once a row's largest exponent is this far above it: at most 2^14
 
-// One element row into its page (a wave): values or keys, slot s.  `live`: older rows s of them.
+// One element row into its page (a wave): values or keys, slot s.  A page that several sequences hold is not written: false.
 template <typename T, int D>
-__device__ __forceinline__ void page_append(const T* row, uint8_t* dst, float* scale, int s, bool values, int lane) {
+__device__ __forceinline__ bool page_append(const T* row, uint8_t* dst, float* scale, const int32_t* refs, int s, bool values, int lane) {
     constexpr int E = D / 64;
+    const int holders = *refs;
     float f[E], most = 0.0f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -691,6 +697,7 @@ __device__ __forceinline__ void page_append(const T* row, uint8_t* dst, float* s
         most = fmaxf(most, finite(f[i]) ? fabsf(f[i]) : 0.0f);
     }
     int e = page_exponent(wave_max(most));
+    if (holders > 1) return false;
     if (s > 0) {
         const int old = exponent_of(*scale);
         if (e > old) {  // the older rows are rounded again
@@ -714,6 +721,7 @@ __device__ __forceinline__ void page_append(const T* row, uint8_t* dst, float* s
 #pragma unroll
     for (int i = 0; i < E; ++i) dst[values ? (lane + 64 * i) * 64 + s : s * D + lane + 64 * i] = encode1(f[i], inv);
     if (lane == 0) *scale = power_of_two(e);
+    return true;
 }
 
 // blockIdx.x = unit * S + split, unit = (layer * B + row) * H + head.  A split is a.chunk pages, shared out to the waves.
@@ -941,7 +949,9 @@ __global__ void __launch_bounds__(NW * kWave, 2) page_step_kernel(const PageArgs
         if ((unsigned)last < (unsigned)a.pages) {
             const int64_t to = ((int64_t)l * a.pages + last) * a.H + h;
             for (int tensor = wv; tensor < 2; tensor += NW)
-                page_append<T, D>(tensor ? vn : kn, (tensor ? a.V : a.K) + to * 64 * D, (tensor ? a.v_scale : a.k_scale) + to, old & 63, tensor != 0, lane);
+                if (!page_append<T, D>(tensor ? vn : kn, (tensor ? a.V : a.K) + to * 64 * D, (tensor ? a.v_scale : a.k_scale) + to, a.refs + last, old & 63,
+                                       tensor != 0, lane) && tensor == 0 && lane == 0)
+                    count_error(a);
         } else if (tid == 0 && (old & 63) == 0) count_error(a);
     }
 }

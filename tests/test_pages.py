@@ -402,6 +402,31 @@ def test_tables_that_are_none_and_rows_without_room():
 
 # ---------------------------------------------------------------- a token's step
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [(kf.BF16, 128), (kf.F16, 64)])
+def test_a_page_that_several_hold_is_not_written(dtype, d):
+    """A reservation that found no page, and rows written all the same: the last full page is the other sequence's too."""
+    L, B, H = 2, 3, 2
+    c, ws, m = both(L, B, H, d, 3, 3, dtype)
+    g = torch.Generator().manual_seed(8)
+    grow(c, ws, m, g, P, [P, 0, P])
+    for x in (c, m):
+        kf.kf_page_fork(x, torch.tensor([0, 0, 2], dtype=torch.int32).cuda(), workspace=ws) if x is c else x.fork([0, 0, 2])
+    grow(c, ws, m, g, 40, [0, 0, 40])  # no page is free now
+    kf.kf_page_reserve(c, 1, torch.tensor([1, 1, 0], dtype=torch.int32).cuda(), workspace=ws)
+    m.reserve(1, [1, 1, 0])
+    m.same(c, ws, "nothing reserved")
+    q, k, v = (rows_of(g, L, B, H, 1, d, dtype).cuda() for _ in range(3))
+    on = torch.tensor([1, 1, 0], dtype=torch.int32).cuda()
+    out = torch.zeros((L, B, H, d), device="cuda")
+    kf.kf_page_step(c, q, k, v, 0.1, out, seq_n=on, workspace=ws)
+    m.errors += L * 2 * H
+    m.same(c, ws, "step")
+    kf.kf_page_write(c, k, v, 1, seq_n=on, workspace=ws)
+    m.errors += L * 2 * H
+    m.same(c, ws, "write")
+
+
+@pytest.mark.gpu
 def test_a_page_number_that_is_none_beside_a_scale_that_is_no_number():
     """The tokens of a page that there is not are left out; what page 0 holds does not come in their place."""
     c, ws, m = both(1, 1, 1, 64, 4, 3)
