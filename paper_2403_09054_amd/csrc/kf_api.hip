@@ -1071,7 +1071,7 @@ static kf_status check_pages(const kf_pages* p, kf::PageArgs* a, size_t* bytes) 
     a->pages = p->pages;
     a->max_pages = p->max_pages;
     const size_t tables = align_up((size_t)p->pages * 4, 256) + align_up((size_t)p->B * 8, 256) + align_up((size_t)p->B * p->max_pages * 4, 256);
-    const int32_t S = kf::page_most_splits(U, p->max_pages);
+    const int32_t S = kf::page_most_splits(U, p->d, p->max_pages);
     const size_t records = S > 1 ? align_up((size_t)U * S * a->G * p->d * 4, 256) + align_up((size_t)U * S * a->G * 8, 256) : 0;
     *bytes = 256 + (tables > records ? tables : records);
     return KF_OK;
@@ -1154,7 +1154,7 @@ kf_status kf_page_step(const kf_pages* p, const void* q, const void* k_new, cons
     a.slopes = alibi_slopes;
     a.seq_n = seq_n;
     a.sc = scale * kf::kLog2e;
-    kf::plan_page_step(&a, U, m_hint ? m_hint : (int32_t)room);
+    kf::plan_page_step(&a, U, p->d, m_hint ? m_hint : (int32_t)room);
     if (U * a.S > kMaxGrid) return fail(KF_EUNSUPPORTED, "%lld units in %d splits each exceed the largest launch", (long long)U, a.S);
     a.ws_o = (float*)((char*)workspace + 256);
     a.ws_ml = (float2*)((char*)workspace + 256 + align_up((size_t)U * a.S * a.G * p->d * 4, 256));

@@ -366,8 +366,8 @@ struct PageArgs {
     int32_t waves;           // of a workgroup of the step
     float sc;                // scale * log2(e)
 };
-int32_t page_most_splits(int64_t U, int32_t max_pages);
-void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint);
+int32_t page_most_splits(int64_t U, int32_t d, int32_t max_pages);
+void plan_page_step(PageArgs* a, int64_t U, int32_t d, int32_t m_hint);
 hipError_t launch_page_step(const PageArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);
 hipError_t launch_page_write(const PageArgs& a, int32_t d, int32_t dtype, hipStream_t stream);
 hipError_t launch_page_reserve(const PageArgs& a, hipStream_t stream);

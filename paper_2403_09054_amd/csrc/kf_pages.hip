@@ -19,7 +19,7 @@ namespace kf {
 
 constexpr int kPageThreads = 256;
 constexpr int kPageWaves = kPageThreads / kWave;
-constexpr int kStepWaves = 4;        // of a workgroup of the step; one where units have a page or two
+constexpr int kStepWaves = 4;        // of a workgroup of the step, or one
 constexpr int kTableThreads = 1024;
 
 typedef __bf16 p_bf2_t __attribute__((ext_vector_type(2)));
@@ -996,20 +996,42 @@ __global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs 
 }
 
 // ---------------------------------------------------------------- launches
-// Splits of a unit's pages: a page a wave at least, and as many workgroups as fill the chip twice.
-int32_t page_most_splits(int64_t U, int32_t max_pages) {
-    int64_t S = (1024 + U - 1) / U;
-    const int64_t most = (max_pages + kStepWaves - 1) / kStepWaves;
-    if (S > most) S = most;
-    if (S > kPageMaxSplits) S = kPageMaxSplits;
-    return (int32_t)(S < 1 ? 1 : S);
+// Workgroups of four waves, or of one, and the splits of a unit's pages.  A wave keeps a page under way, so that one or two waves a SIMD, 1024
+// to 2048 of them (twice as many with rows half as long), are what the memory asks for.
+// As many units take one wave each (2048 units x 1000 x 128: 95 us, with four waves each 110; x 60: 18 and 29), of long ones up to four splits, lest
+// a long unit among short ones is one chain; from half as many on two waves each where pages pay for the join (640 units x 1300: 44 us, with
+// four waves each 51).  Fewer units take four waves and as many splits as make up to 512 workgroups (512 units x 1024 x 128: 29 us, two splits
+// 35, two of one wave 34), a page a wave at least; long units, whose splits cost little, as many as hold 24 pages each, up to 1024
+// workgroups (48 units of up to 31833 tokens: 58 us with 22 splits each, 61 with 20, 90 with 6).
+static int32_t page_splits(int64_t U, int32_t d, int32_t pages, int32_t* waves) {
+    const int64_t full = d == 64 ? 2048 : 1024;
+    *waves = U >= full || (U > full / 2 && (d > 64 || pages >= 8 || pages <= 2)) ? 1 : kStepWaves;
+    int64_t S;
+    if (*waves == 1) {
+        S = (pages + 63) / 64 < 4 ? (pages + 63) / 64 : 4;
+        if (U < full && pages >= 8 && S < 2) S = 2;
+    } else {
+        const int64_t even = full / 2 / U, parts = pages / 24, fill = (full + U - 1) / U, most = (pages + kStepWaves - 1) / kStepWaves;
+        S = parts < fill ? parts : fill;
+        if (S < even) S = even;
+        if (S < 1) S = 1;
+        if (S > most) S = most;
+        if (S > kPageMaxSplits) S = kPageMaxSplits;
+    }
+    return (int32_t)S;
 }
-void plan_page_step(PageArgs* a, int64_t U, int32_t m_hint) {
-    const int32_t pages = (m_hint + 63) / 64;
-    const int32_t S = page_most_splits(U, pages);
+// Bounds the splits of plan_page_step for any hint.
+int32_t page_most_splits(int64_t U, int32_t d, int32_t max_pages) {
+    int32_t waves;
+    const int32_t S = page_splits(U, d, max_pages, &waves);
+    return waves == 1 ? S : (5 * S + 3) / 4 < kPageMaxSplits ? (5 * S + 3) / 4 : kPageMaxSplits;
+}
+void plan_page_step(PageArgs* a, int64_t U, int32_t d, int32_t m_hint) {
+    const int32_t pages = (m_hint + 63) / 64, S = page_splits(U, d, pages, &a->waves);
     a->chunk = (pages + S - 1) / S;
+    // whole rounds of the waves; five pages would be two (58 units x 2518 x 256, 8 heads: 30 us, of four pages 25)
+    if (a->waves == kStepWaves && S > 1) a->chunk = a->chunk == kStepWaves + 1 && S * 5 / 4 < kPageMaxSplits ? kStepWaves : (a->chunk + kStepWaves - 1) / kStepWaves * kStepWaves;
     a->S = (pages + a->chunk - 1) / a->chunk;
-    a->waves = a->S == 1 && (pages == 1 || (pages == 2 && U >= 512)) ? 1 : kStepWaves;
 }
 
 template <typename T, int D>
