@@ -531,18 +531,26 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
     const int parts = a.ws_parts[unit * a.tiles + R / a.block_rows];
     if (parts == 1) return;
     const int64_t row = at * a.S;
-    float m = -INFINITY;
-    for (int s = 0; s < parts; ++s) m = fmaxf(m, a.ws_ml[row + s].x);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, x[E];
+    // at most 64 parts: a lane a part's reference and sum, and the rows of sums come in one trip (eight at a time)
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    if (lane < parts) ml = a.ws_ml[row + lane];
+    const float m = wave_max(ml.x), by = hw_exp2(ml.x - (m == -INFINITY ? 0.0f : m));
+    const float l = wave_sum(lane < parts ? by * ml.y : 0.0f);
+    float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    for (int s = 0; s < parts; ++s) {
-        const float2 ml = a.ws_ml[row + s];
-        const float by = hw_exp2(ml.x - ref);
-        l = fmaf(by, ml.y, l);
+    for (int s = 0; s < parts; s += 8) {
+        float v[8][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(by, a.ws_o[(row + s) * D + lane * E + e], x[e]);
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[i][e] = a.ws_o[(row + min(s + i, parts - 1)) * D + lane * E + e];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float w = s + i < parts ? __shfl(by, s + i, kWave) : 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = fmaf(w, s + i < parts ? v[i][e] : 0.0f, x[e]);
+        }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     T* w = (T*)a.out + (a.q_start ? q0 * a.o_st : b * a.o_sb) + qh * a.o_sh + qi * a.o_st + lane * E;
@@ -572,15 +580,20 @@ enum { kAttendMany, kAttendFewer, kAttendOne, kAttendFew };
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
     const int64_t units = (int64_t)a->B * a->H, rows = (int64_t)a->n * a->G, b64 = units * ((rows + 63) / 64);
     const bool wide = d * (dtype == KF_F32 ? 4 : 2) > 256;
+    a->shape = kAttendFewer;
     if (units * ((rows + 127) / 128) >= (wide ? 512 : 1024)) a->shape = kAttendMany;
-    else if (wide || b64 > 256) a->shape = kAttendFewer;
-    else a->shape = b64 > 64 ? kAttendOne : kAttendFew;
+    else if (!wide && a->m > 512 && rows <= 32 && units <= 64) a->shape = kAttendFew;
+    else if (!wide && a->m > 512 && b64 > 64 && b64 <= 256) a->shape = kAttendOne;
     a->block_rows = a->shape == kAttendMany ? 128 : a->shape == kAttendFew ? 32 : 64;
     a->tiles = (int32_t)((rows + a->block_rows - 1) / a->block_rows);
     a->S = 1;
     const int64_t blocks = units * a->tiles;
-    int64_t S = 256 / blocks;
-    if (S > a->m / 512) S = a->m / 512;
+    // Few workgroups share out the keys: a part costs the join as much as ten keys of a walk, and a row's record as much as a sixteenth of one.
+    // (8 x 1 row x 1000 keys, 128 bf16: one part 15.6 us, parts of 128 keys 11.6; 2 x 1 x 8000: 66.6, 62 parts 15.9, 27 14; 8 x 1024 x 1024:
+    // one part 17.9, two 21.1; 8 x 512 x 2048: 28.7, four 20.5.)
+    int64_t least = (int64_t)sqrt(10.0 * a->m) + units * rows / 16, S = 256 / blocks;
+    if (least < kFarTile) least = kFarTile;
+    if (S > a->m / least) S = a->m / least;
     if (S > 64) S = 64;
     if (S > 1) {
         a->chunk = (int32_t)(((a->m + S - 1) / S + 127) / 128 * 128);
