@@ -1000,37 +1000,42 @@ __global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs 
 // to 2048 of them (twice as many with rows half as long), are what the memory asks for.
 // As many units take one wave each (2048 units x 1000 x 128: 95 us, with four waves each 110; x 60: 18 and 29), of long ones up to four splits, lest
 // a long unit among short ones is one chain; from half as many on two waves each where pages pay for the join (640 units x 1300: 44 us, with
-// four waves each 51).  Fewer units take four waves and as many splits as make up to 512 workgroups (512 units x 1024 x 128: 29 us, two splits
-// 35, two of one wave 34), a page a wave at least; long units, whose splits cost little, as many as hold 24 pages each, up to 1024
-// workgroups (48 units of up to 31833 tokens: 58 us with 22 splits each, 61 with 20, 90 with 6).
-static int32_t page_splits(int64_t U, int32_t d, int32_t pages, int32_t* waves) {
-    const int64_t full = d == 64 ? 2048 : 1024;
-    *waves = U >= full || (U > full / 2 && (d > 64 || pages >= 8 || pages <= 2)) ? 1 : kStepWaves;
+// four waves each 51).  Fewer units take four waves and as many splits as make up to 512 workgroups, which all run at once (512 units x 1024 x 128: 29 us,
+// two splits 35, two of one wave 34), a page a wave at least; long units, whose splits cost little, as many as hold 24 pages each, up to 1024
+// workgroups (48 units of up to 31833 tokens: 58 us with 22 splits each, 90 with 6), where the 256 compute units get as many each (32 units x 32768: 16
+// splits each 48 us, 19 splits 65, 32 splits 49; 288 x 6484: one split 114, four 90).
+static int32_t page_splits(int64_t U, int32_t d, int32_t pages, int32_t* waves, bool bound) {
+    const int64_t full = d == 64 ? 2048 : 1024, round = full / 2;
+    *waves = U >= full || (U > round && (d > 64 || pages >= 8 || pages <= 2)) ? 1 : kStepWaves;
     int64_t S;
     if (*waves == 1) {
         S = (pages + 63) / 64 < 4 ? (pages + 63) / 64 : 4;
         if (U < full && pages >= 8 && S < 2) S = 2;
-    } else {
-        const int64_t even = full / 2 / U, parts = pages / 24, fill = (full + U - 1) / U, most = (pages + kStepWaves - 1) / kStepWaves;
-        S = parts < fill ? parts : fill;
-        if (S < even) S = even;
-        if (S < 1) S = 1;
-        if (S > most) S = most;
-        if (S > kPageMaxSplits) S = kPageMaxSplits;
+        return (int32_t)S;
     }
-    return (int32_t)S;
+    const int64_t parts = pages / 24, fill = (full + U - 1) / U, most = (pages + kStepWaves - 1) / kStepWaves;
+    const int64_t low = round / U < 1 ? 1 : round / U, high = parts < fill ? parts : fill;
+    S = high > low ? high : low;
+    if (!bound) {                                // the most splits that keep the compute units nearly as busy as can be
+        auto busy = [&](int64_t x) { return U * x < 256 ? 1.0 : (double)(U * x) / (double)((U * x + 255) / 256 * 256); };
+        double best = 0.0;
+        for (int64_t x = low; x <= S; ++x) best = busy(x) > best ? busy(x) : best;
+        while (S > low && busy(S) < 0.9 * best) --S;
+    }
+    if (S > most) S = most;
+    return (int32_t)(S > kPageMaxSplits ? kPageMaxSplits : S);
 }
 // Bounds the splits of plan_page_step for any hint.
 int32_t page_most_splits(int64_t U, int32_t d, int32_t max_pages) {
     int32_t waves;
-    const int32_t S = page_splits(U, d, max_pages, &waves);
+    const int32_t S = page_splits(U, d, max_pages, &waves, true);
     return waves == 1 ? S : (5 * S + 3) / 4 < kPageMaxSplits ? (5 * S + 3) / 4 : kPageMaxSplits;
 }
 void plan_page_step(PageArgs* a, int64_t U, int32_t d, int32_t m_hint) {
-    const int32_t pages = (m_hint + 63) / 64, S = page_splits(U, d, pages, &a->waves);
+    const int32_t pages = (m_hint + 63) / 64, S = page_splits(U, d, pages, &a->waves, false);
     a->chunk = (pages + S - 1) / S;
-    // whole rounds of the waves; five pages would be two (58 units x 2518 x 256, 8 heads: 30 us, of four pages 25)
-    if (a->waves == kStepWaves && S > 1) a->chunk = a->chunk == kStepWaves + 1 && S * 5 / 4 < kPageMaxSplits ? kStepWaves : (a->chunk + kStepWaves - 1) / kStepWaves * kStepWaves;
+    // a fifth page would be a second round of one wave (58 units x 2518 x 256, 8 heads: 30 us, with four pages 25)
+    if (a->waves == kStepWaves && a->chunk == kStepWaves + 1 && S > 1 && S * 5 / 4 < kPageMaxSplits) a->chunk = kStepWaves;
     a->S = (pages + a->chunk - 1) / a->chunk;
 }
 
