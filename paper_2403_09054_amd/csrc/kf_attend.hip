@@ -8,7 +8,18 @@
 // all of them -- and forms S^T = K Q^T and O^T = V^T P^T in tiles of 32 x 32: a lane then owns one row in both, its maximum and sum
 // need one exchange between the wave's halves, and the exponentials, rounded to the element type, are the second product's operand as
 // they lie.  (The order of the keys inside a product is free; the values' operand is read transposed from LDS in the same order.)
-// Tiles of K and V go from memory through registers into LDS, two buffers, swizzled so that both ways of reading meet each bank once.
+// Tiles of K and V go from memory straight to LDS, two buffers, swizzled so that both ways of reading meet each bank once.
+//
+// What bounds it: many rows, the matrix cores beside the vector unit (128 elements a row: 512 operations of the one for each exponential,
+// sum and rounding of the other), and the power they draw.  8 x 32 heads x 4096 x 128 bf16, causal: 1180 us, 930 TFLOP/s (a product of
+// 8192^3: 1155 to 1394); with a position bias, far tiles left out, 830; 8 heads of 8 x 512 rows at the end of 8192 keys 500 us, 1070 TFLOP/s; 256
+// elements 760, 64 elements 760, fp32 59 (its own products' rate).  Counters: no bank conflicts in LDS, matrix cores busy 40 % of the cycles at 2.0
+// GHz; inputs of zeros run 10 % faster.  Few rows: the chain of a walk, 8 us for 1000 keys, and the join; 16 x 2048 x 128 40 us.
+//
+// Steps of 8 x 32 x 4096 x 128: tiles by way of registers, which spilled, 3133 us; infinities and NaNs of edge tiles taken out in LDS instead
+// of beside every product 1328; direct loads to LDS 1245; keys a step ahead of the values 1190.  Tried, no gain: tiles of 32 keys (3 to 5 % more),
+// workgroups of 256 rows (5 % less for 16384 keys, more for causal ones of 4096), wave priorities, three or four buffers, orders of
+// instructions laid down by hand, two accumulators a block of logits (8 % more).
 #include "kf_device.h"
 #include "kf_internal.h"
 #include "kf_prefill.h"
@@ -562,7 +573,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
 }
 
 // Shapes of a workgroup, by the bytes of a row: for many rows; for fewer; for about a workgroup of 64 rows a compute unit, whose waves are twice
-// as many; for a few rows.
+// as many; for rows of a single wave.  Rows of 512 bytes fill registers and LDS with less.
 template <int RB>
 struct AttendShapes {
     using Many = AttendShape<4, 1, RB == 256 ? 2 : 1, 2>;
@@ -580,6 +591,10 @@ enum { kAttendMany, kAttendFewer, kAttendOne, kAttendFew };
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
     const int64_t units = (int64_t)a->B * a->H, rows = (int64_t)a->n * a->G, b64 = units * ((rows + 63) / 64);
     const bool wide = d * (dtype == KF_F32 ? 4 : 2) > 256;
+    // 128 rows a workgroup where there are four rounds of them (two of wide rows): 32 heads x 4096 x 128 167 us, with 64 rows 174, 32 x 2048 63 and 59,
+    // 16 x 4096 x 256 180 and 220, 16 x 2048 x 256 83 and 70.  64 rows and eight waves where these are a round at most and walks are long: 16 x
+    // 2048 x 128 37 us, with four waves 40, 8 x 2048 26.5 and 30, but 32 x 1024 32 and 25; 16 x 16 sequences of 64 11 and 8.  A wave of rows: 2
+    // heads x 1 x 8000 14.7 us, with two waves of them 15.2, 4 x (20 rows of 2 heads) x 5000 x 64 13.0 and 13.8.
     a->shape = kAttendFewer;
     if (units * ((rows + 127) / 128) >= (wide ? 512 : 1024)) a->shape = kAttendMany;
     else if (!wide && a->m > 512 && rows <= 32 && units <= 64) a->shape = kAttendFew;
@@ -599,11 +614,14 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
         a->chunk = (int32_t)(((a->m + S - 1) / S + 127) / 128 * 128);
         a->S = (a->m + a->chunk - 1) / a->chunk;
     }
+    // (20 heads x 2048 x 128: 47 us, a head after the other 62; 3 x 12 x 2900 120 and 125.)
     a->spread = 1;
     while (units * a->spread % kXcds) a->spread *= 2;
     if (a->H % kXcds == 0 || a->tiles < 4 * a->spread) a->spread = 1;
     a->blocks = units * a->spread * ((a->tiles + a->spread - 1) / a->spread) * a->S;  // of the launch
-    // A row of far tiles is looked for where a key is read often enough: the search reads K and V once more.
+    // A row of far tiles is looked for where a key is read often enough: the search is a launch that reads K and V once more, 95 of 835 us of
+    // 8 x 32 x 4096 x 128, which take 1350 without.  4 x 32 x 4096 430 and 665 us, 32 x 2048 57 and 67, 8 x 4096 72 and 70, 8 x 2048 37 and 32 (few
+    // workgroups, which wait for the head of the gentlest slope); 8 x 32 x 1024 136 with it and 132.
     a->far_tiles = a->slopes && (int64_t)a->n * a->G >= 2048 && units <= 65535 ? (a->m + kFarTile - 1) / kFarTile : 0;
     a->ws_rows = a->S > 1 ? blocks * a->block_rows : 0;
 }

@@ -12,6 +12,13 @@
 // query head, twice: once for the upper 11 bits of its probabilities and once for the rest, so that out keeps 22 bits of them.  Which
 // token is which row of a tile is free: a lane's four tiles hold 16 neighbouring tokens, and 16 bytes of a row of V are the operand of
 // two products.
+//
+// What bounds them: the bytes.  The step reads a page at 6.5 TB/s (2048 units x 4096 x 128: 331 us; a layer of 64 x 32 of 512 to 2048 tokens
+// 131 us, 4.5; 32 units x 32768 49 us, 5.5; 8 units x 1501, 4 heads each: 10.4, two launches).  Steps of the first: pages
+// looked up by the vector unit 382 us, by the scalar unit and the first ahead of the token 368, a wave a unit instead of four 331.  Tried: three workgroups a compute unit (registers spill),
+// 2048 or 4096 workgroups (slower), workgroups of two waves (7 % more).  Rows in: 5.8 TB/s read and written (32 heads x 32768 x 128: 138 us).  Forks and
+// reservations are launches of one workgroup, a chain of trips; kept rows are gathered a byte of V at a time (256 units of 2048 tokens, 1024 kept: 171 us,
+// 3.1 TB/s).
 #include "kf_device.h"
 #include "kf_internal.h"
 
@@ -376,7 +383,8 @@ __global__ void __launch_bounds__(kTableThreads) page_shrink_kernel(const PageAr
 __device__ __forceinline__ float block_most(float v, float* red) { return block_max<kPageThreads>(v, red); }
 
 // A workgroup a new page of a head.  Keys: 16-byte pieces of rows.  Values: a wave's lanes are the page's tokens, a load a
-// byte of each; a sequence's tokens are in order, so that a load falls on few lines.
+// byte of each; a sequence's tokens are in order, so that a load falls on few lines.  Bound by these loads: 171 us where the bytes take 112.
+// Tried: old rows of V whole in LDS (373 us: half of what a page holds is not kept), heads of a page on one XCD (296; the head fastest 164 to 171).
 template <int D>
 __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs a) {
     __shared__ int page_s[64], slot_s[64];
