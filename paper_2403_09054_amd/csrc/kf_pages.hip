@@ -17,8 +17,8 @@
 // 131 us, 4.5; 32 units x 32768 49 us, 5.5; 8 units x 1501, 4 heads each: 10.4, two launches).  Steps of the first: pages
 // looked up by the vector unit 382 us, by the scalar unit and the first ahead of the token 368, a wave a unit instead of four 331.  Tried: three workgroups a compute unit (registers spill),
 // 2048 or 4096 workgroups (slower), workgroups of two waves (7 % more).  Rows in: 5.8 TB/s read and written (32 heads x 32768 x 128: 138 us).  Forks and
-// reservations are launches of one workgroup, a chain of trips; kept rows are gathered a byte of V at a time (256 units of 2048 tokens, 1024 kept: 171 us,
-// 3.1 TB/s).
+// reservations are launches of one workgroup, a chain of trips; kept rows are gathered a byte of V at a time (1024 units of 2048 tokens, 1024 kept: 177 us,
+// 3.0 TB/s).
 #include "kf_device.h"
 #include "kf_internal.h"
 
@@ -383,8 +383,9 @@ __global__ void __launch_bounds__(kTableThreads) page_shrink_kernel(const PageAr
 __device__ __forceinline__ float block_most(float v, float* red) { return block_max<kPageThreads>(v, red); }
 
 // A workgroup a new page of a head.  Keys: 16-byte pieces of rows.  Values: a wave's lanes are the page's tokens, a load a
-// byte of each; a sequence's tokens are in order, so that a load falls on few lines.  Bound by these loads: 171 us where the bytes take 112.
-// Tried: old rows of V whole in LDS (373 us: half of what a page holds is not kept), heads of a page on one XCD (296; the head fastest 164 to 171).
+// byte of each; a sequence's tokens are in order, so that a load falls on few lines.  Bound by these loads: a pass of 177 us where the bytes take 112.
+// Tried: old rows of V whole in LDS (373 us: half of what a page holds is not kept), heads of a page on one XCD (296); whole words of the
+// rows of up to four pages, whose bytes are exchanged between lanes (168, and 3 to 6 % more where less is kept).
 template <int D>
 __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs a) {
     __shared__ int page_s[64], slot_s[64];
@@ -396,13 +397,15 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
     const unsigned pages = (unsigned)(a.kept + 63) / 64, rest = blockIdx.x / (unsigned)a.H;
     const int h = (int)(blockIdx.x - rest * (unsigned)a.H), lb = (int)(rest / pages), j = (int)(rest - (unsigned)lb * pages);
     const int l = lb / a.B, b = lb - l * a.B, j0 = j * 64;
-    const int n = a.ws_copy[b].x;
-    if (n == 0) return;
+    // trips to memory in a row: the sequence, the kept tokens and the new page; the tokens' pages; their codes beside their scales
     const int live = min(64, a.kept - j0);
+    const int s = a.keep[((int64_t)lb * a.H + h) * a.kept + j0 + min(lane, live - 1)];
+    const int n = uniform_load(&a.ws_copy[b].x), fresh = uniform_load(a.table + (int64_t)b * a.max_pages + j);
+    if (n == 0) return;
+    float ks = 0.0f, vs = 0.0f;
     if (tid < 64) {
         int page = -1, slot = 0;
         if (tid < live) {
-            const int s = a.keep[((int64_t)lb * a.H + h) * a.kept + j0 + tid];
             if ((unsigned)s < (unsigned)n) {
                 page = a.ws_old[(int64_t)b * a.max_pages + (s >> 6)];
                 slot = s & 63;
@@ -410,11 +413,13 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
         }
         page_s[tid] = page;
         slot_s[tid] = slot;
-        ks_s[tid] = page < 0 ? 0.0f : a.k_scale[((int64_t)l * a.pages + page) * a.H + h];
-        vs_s[tid] = page < 0 ? 0.0f : a.v_scale[((int64_t)l * a.pages + page) * a.H + h];
+        if (page >= 0) {
+            ks = a.k_scale[((int64_t)l * a.pages + page) * a.H + h];
+            vs = a.v_scale[((int64_t)l * a.pages + page) * a.H + h];
+        }
     }
     __syncthreads();
-    const int64_t tile = 64 * D, to = ((int64_t)l * a.pages + a.table[(int64_t)b * a.max_pages + j]) * a.H + h;
+    const int64_t tile = 64 * D, to = ((int64_t)l * a.pages + fresh) * a.H + h;
     const int64_t layer = (int64_t)l * a.pages;
     constexpr int CH = D / 16, PT = 64 * CH / kPageThreads, ROWS = D / kPageWaves;  // rows of values of a wave
     uint8_t vc[ROWS];
@@ -433,6 +438,8 @@ __global__ void __launch_bounds__(kPageThreads) page_keep_kernel(const PageArgs 
             c[x] = make_uint4(0u, 0u, 0u, 0u);
             if (page_s[t] >= 0) c[x] = *(const uint4*)(a.K + ((layer + page_s[t]) * a.H + h) * tile + slot_s[t] * D + p % CH * 16);
         }
+        if (tid < 64) ks_s[tid] = ks, vs_s[tid] = vs;
+        __syncthreads();
 #pragma unroll
         for (int x = 0; x < PT; ++x) {
             const float s = ks_s[(tid + x * kPageThreads) / CH];
@@ -514,7 +521,7 @@ __global__ void __launch_bounds__(kPageThreads) page_write_kernel(const PageArgs
     const int column = (int)threadIdx.x % CH;
     __shared__ float red[kPageWaves];
     const int tid = threadIdx.x;
-    const unsigned pages = (unsigned)(a.n + 62) / 64 + 1, rest = blockIdx.x / (unsigned)a.H;
+    const unsigned pages = ((unsigned)a.n + 62u) / 64 + 1, rest = blockIdx.x / (unsigned)a.H;
     const int h = (int)(blockIdx.x - rest * (unsigned)a.H), lb = (int)(rest / pages), jx = (int)(rest - (unsigned)lb * pages);
     const int l = lb / a.B, b = lb - l * a.B;
     const int add = a.seq_n ? a.seq_n[b] : a.n, len = a.len[b];
