@@ -710,3 +710,55 @@ def test_a_search_over_pages_from_prompt_to_tokens():
     m.same(c, ws, "kept")
     take_step(c, ws, m, g)
     m.same(c, ws, "after")
+
+
+@pytest.mark.gpu
+def test_thousands_of_sequences():
+    """More rows of the table than a workgroup has threads, and fewer pages than they ask for."""
+    L, B, H, d = 1, 2500, 1, 64
+    c, ws, m = both(L, B, H, d, 2300, 2)
+    g = torch.Generator().manual_seed(11)
+    counts = [int(x) for x in torch.randint(0, 90, (B,), generator=g)]
+    kf.kf_page_reserve(c, 80, torch.tensor(counts, dtype=torch.int32).cuda(), workspace=ws)
+    m.reserve(80, counts)
+    m.same(c, ws, "reserved")
+    assert m.errors > 0 and 0 < min(x for x in m.len if x) < 80  # some found no page, of those behind them some did
+    x = rows_of(g, L, B, H, 80, d, kf.BF16)
+    held = [n if 1 <= n <= 80 and m.len[b] == n else 0 for b, n in enumerate(counts)]
+    kf.kf_page_write(c, x.cuda(), x.cuda(), 80, seq_n=torch.tensor(held, dtype=torch.int32).cuda(), workspace=ws)
+    m.write(x.double().numpy(), x.double().numpy(), held)
+    which = [int(b % 3 == 0) for b in range(B)]
+    kf.kf_page_free(c, torch.tensor(which, dtype=torch.int32).cuda(), workspace=ws)
+    m.free(which)
+    parent = [b if b % 3 else b + 1 if b + 1 < B else b for b in range(B)]
+    kf.kf_page_fork(c, torch.tensor(parent, dtype=torch.int32).cuda(), workspace=ws)
+    m.fork(parent)
+    m.same(c, ws, "forked")
+    keep = torch.randint(0, 5, (L, B, H, 5), generator=g, dtype=torch.int32)
+    kf.kf_page_compact(c, keep.cuda(), 5, workspace=ws)
+    m.compact(keep.numpy(), 5, [1] * B)
+    m.same(c, ws, "compacted")
+
+
+@pytest.mark.gpu
+def test_two_caches_on_two_streams():
+    """Calls at once, each cache with a workspace of its own: as one after the other."""
+    g = torch.Generator().manual_seed(12)
+    sets = []
+    for lens in ([900, 1300, 20], [1200, 64, 700]):
+        c, ws, m = both(1, 3, 4, 128, 64, 32, kf.BF16, 2)
+        fill(c, ws, m, g, lens)
+        q, k, v = (torch.randn((1, 3, h, 128), generator=g).bfloat16().cuda() for h in (8, 4, 4))
+        sets.append((c, ws, q, k, v, [torch.zeros((1, 3, 8, 128), device="cuda") for _ in range(2)]))
+    torch.cuda.synchronize()
+    for c, ws, q, k, v, out in sets:
+        kf.kf_page_step(c, q, k, v, 0.1, out[0], workspace=ws)  # (the last token's place each time: nothing is reserved)
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, (c, ws, q, k, v, out) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                kf.kf_page_step(c, q, k, v, 0.1, out[1], workspace=ws)
+    torch.cuda.synchronize()
+    for c, ws, q, k, v, out in sets:
+        assert bool(out[0].any()) and torch.equal(out[0], out[1]) and int(ws[:4].view(torch.int32)) == 0

@@ -407,3 +407,24 @@ def test_a_prompts_layer_from_projection_to_reduced_cache():
         want, tol = oracle(Q[b, :, :lens[b]].cpu(), stage.K[0, b, :, :lens[b]].cpu(), stage.V[0, b, :, :lens[b]].cpu(), d ** -0.5, None, G, torch.bfloat16)
         near(out[b, :lens[b]].transpose(0, 1), want, tol, b)
         assert bool((out[b, lens[b]:] == 0).all())
+
+
+@pytest.mark.gpu
+def test_calls_at_once_and_twice_are_the_same_to_the_bit():
+    """Two prompts on two streams with a workspace each, over and over: shared-out keys, far keys and whole walks."""
+    g, calls = torch.Generator().manual_seed(4), []
+    for B, n, m, H, G, slopes in ((2, 30, 3000, 4, 2, None), (1, 2100, 2100, 2, 1, slopes_of(2).cuda()), (3, 500, 500, 8, 1, None)):
+        Q, K, V = (torch.randn((B, h, r, 128), generator=g).bfloat16().cuda() for h, r in ((H * G, n), (H, m), (H, m)))
+        p = kf.Prompt(B, n, m, H, 128, kf.BF16, 0.09, q_per_kv=G, slopes=slopes)
+        out = [torch.zeros((B, n, H * G, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        calls.append((p, (Q, K, V), out, kf.new_prompt_workspace(p)))
+        kf.kf_prompt_attend(p, Q, K, V, out[0], workspace=calls[-1][3])
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, (p, x, out, ws) in zip(streams, calls):
+            with torch.cuda.stream(s):
+                kf.kf_prompt_attend(p, *x, out[1], workspace=ws)
+    torch.cuda.synchronize()
+    for p, x, out, ws in calls:
+        assert bool(out[0].any()) and torch.equal(out[0], out[1])
