@@ -473,8 +473,9 @@ kf_status kf_prompt_attend(const kf_prompt *p, const void *Q, const void *K, con
  * Pages are taken lowest number first, sequences in order.  table, len and refs serve all layers; a caller that runs its layers one
  * after the other passes the struct with L = 1 and the layer's K, V and scales to kf_page_write and kf_page_step.
  * dtype (KF_BF16 or KF_F16) is that of the rows that go in and of the queries.  d: 64, 128 or 256; q_per_kv: 1, 2, 4 or 8; B up to 8192.
- * The workspace (kf_page_workspace_bytes, by the whole struct or one layer of it) is DEVICE memory, 16-byte aligned; only its first
- * word must start as zero: it counts sequences, or pages of a unit, that a kernel had to leave out.
+ * The workspace is DEVICE memory, 16-byte aligned; only its first word must start as zero: it counts sequences, or pages of a unit, that a
+ * kernel had to leave out.  What kf_page_workspace_bytes says of a struct serves every call on it and on any number of its layers; what it says of
+ * one layer serves the steps of one layer, and the other calls on all of them.
  */
 #define KF_PAGE_TOKENS 64
 typedef struct {

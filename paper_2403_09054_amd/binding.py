@@ -535,7 +535,7 @@ def kf_page_workspace_bytes(pages: Pages) -> int:
 
 
 def new_page_workspace(pages: Pages, device="cuda"):
-    """A zero-filled workspace tensor for every call on these pages."""
+    """A zero-filled workspace tensor for every call on these pages, and on their layers one by one."""
     import torch
     nbytes = kf_page_workspace_bytes(pages)
     if nbytes == 0:

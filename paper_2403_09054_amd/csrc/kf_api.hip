@@ -1043,8 +1043,16 @@ kf_status kf_prompt_attend(const kf_prompt* p, const void* Q, const void* K, con
 }
 
 // Workspace of the page calls: the error word, then, for one call at a time, the free pages that go out, what is copied and the
-// table before, or the records of a step's splits.
-static kf_status check_pages(const kf_pages* p, kf::PageArgs* a, size_t* bytes) {
+// table before (whatever the layers), or the records of a step's splits.
+static size_t page_tables(const kf_pages* p) {
+    return align_up((size_t)p->pages * 4, 256) + align_up((size_t)p->B * 8, 256) + align_up((size_t)p->B * p->max_pages * 4, 256);
+}
+static size_t page_records(const kf_pages* p, int64_t layers) {
+    const int64_t U = layers * p->B * p->H, G = p->q_per_kv > 1 ? p->q_per_kv : 1;
+    const int32_t S = kf::page_most_splits(U, p->d, p->max_pages);
+    return S > 1 ? align_up((size_t)U * S * G * p->d * 4, 256) + align_up((size_t)U * S * G * 8, 256) : 0;
+}
+static kf_status check_pages(const kf_pages* p, kf::PageArgs* a) {
     if (!p) return fail(KF_EINVAL, "pages description is NULL");
     if (p->L < 1 || p->B < 1 || p->H < 1 || p->d < 1 || p->pages < 1 || p->max_pages < 1)
         return fail(KF_EINVAL, "sizes must be positive (L=%d B=%d H=%d d=%d pages=%d max_pages=%d)", p->L, p->B, p->H, p->d, p->pages, p->max_pages);
@@ -1070,21 +1078,16 @@ static kf_status check_pages(const kf_pages* p, kf::PageArgs* a, size_t* bytes) 
     a->G = p->q_per_kv > 1 ? p->q_per_kv : 1;
     a->pages = p->pages;
     a->max_pages = p->max_pages;
-    const size_t tables = align_up((size_t)p->pages * 4, 256) + align_up((size_t)p->B * 8, 256) + align_up((size_t)p->B * p->max_pages * 4, 256);
-    const int32_t S = kf::page_most_splits(U, p->d, p->max_pages);
-    const size_t records = S > 1 ? align_up((size_t)U * S * a->G * p->d * 4, 256) + align_up((size_t)U * S * a->G * 8, 256) : 0;
-    *bytes = 256 + (tables > records ? tables : records);
     return KF_OK;
 }
 
-// The checks of a call that launches, and the workspace's places.
-static kf_status begin_pages(const kf_pages* p, kf::PageArgs* a, void* workspace, size_t workspace_bytes) {
-    size_t bytes;
-    const kf_status st = check_pages(p, a, &bytes);
+// The checks of a call that launches, and the workspace's places; a step asks for its records, the other calls for tables.
+static kf_status begin_pages(const kf_pages* p, kf::PageArgs* a, void* workspace, size_t workspace_bytes, bool step = false) {
+    const kf_status st = check_pages(p, a);
     if (st != KF_OK) return st;
     if (!p->K || !p->V || !p->k_scale || !p->v_scale || !p->table || !p->len || !p->refs) return fail(KF_EINVAL, "pages have a NULL buffer");
     if (((uintptr_t)p->K | (uintptr_t)p->V) & 15) return fail(KF_EINVAL, "K and V must be 16-byte aligned");
-    const kf_status ws = check_ws(workspace, workspace_bytes, bytes);
+    const kf_status ws = check_ws(workspace, workspace_bytes, 256 + (step ? page_records(p, p->L) : page_tables(p)));
     if (ws != KF_OK) return ws;
     char* w = (char*)workspace;
     a->ws_err = (int32_t*)w + KF_WS_ERROR_WORD;
@@ -1104,8 +1107,16 @@ static kf_status end_pages(hipError_t e, const char* what) {
 
 size_t kf_page_workspace_bytes(const kf_pages* p) {
     kf::PageArgs a;
-    size_t bytes;
-    return check_pages(p, &a, &bytes) == KF_OK ? bytes : 0;
+    if (check_pages(p, &a) != KF_OK) return 0;
+    // For the struct and any number of its layers: fewer units take more splits each, so that the records of a layer can be more than
+    // those of all.  From kPageMostCut units on the splits of a unit depend on its pages alone.
+    size_t bytes = page_tables(p), r = page_records(p, p->L);
+    if (r > bytes) bytes = r;
+    for (int64_t l = 1; l < p->L && l * p->B * p->H < kf::kPageMostCut; ++l) {
+        r = page_records(p, l);
+        if (r > bytes) bytes = r;
+    }
+    return 256 + bytes;
 }
 
 kf_status kf_page_reserve(const kf_pages* p, int32_t n, const int32_t* seq_n, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1139,7 +1150,7 @@ kf_status kf_page_write(const kf_pages* p, const void* k, const void* v, int32_t
 kf_status kf_page_step(const kf_pages* p, const void* q, const void* k_new, const void* v_new, float scale, const float* alibi_slopes,
                        const int32_t* seq_n, int32_t m_hint, float* out, void* workspace, size_t workspace_bytes, void* stream) {
     kf::PageArgs a;
-    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes);
+    const kf_status st = begin_pages(p, &a, workspace, workspace_bytes, true);
     if (st != KF_OK) return st;
     if (!q || !k_new || !v_new || !out) return fail(KF_EINVAL, "q, k_new, v_new and out must not be NULL");
     if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return fail(KF_EINVAL, "q, k_new and v_new must be 16-byte aligned");

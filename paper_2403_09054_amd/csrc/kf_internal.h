@@ -366,6 +366,7 @@ struct PageArgs {
     int32_t waves;           // of a workgroup of the step
     float sc;                // scale * log2(e)
 };
+constexpr int32_t kPageMostCut = 2048;  // units from which on a unit's splits do not depend on how many there are
 int32_t page_most_splits(int64_t U, int32_t d, int32_t max_pages);
 void plan_page_step(PageArgs* a, int64_t U, int32_t d, int32_t m_hint);
 hipError_t launch_page_step(const PageArgs& a, int64_t U, int32_t d, int32_t dtype, hipStream_t stream);

@@ -1020,7 +1020,7 @@ __global__ void __launch_bounds__(kPageThreads) page_join_kernel(const PageArgs 
 // workgroups (48 units of up to 31833 tokens: 58 us with 22 splits each, 90 with 6), where the 256 compute units get as many each (32 units x 32768: 16
 // splits each 48 us, 19 splits 65, 32 splits 49; 288 x 6484: one split 114, four 90).
 static int32_t page_splits(int64_t U, int32_t d, int32_t pages, int32_t* waves, bool bound) {
-    const int64_t full = d == 64 ? 2048 : 1024, round = full / 2;
+    const int64_t full = d == 64 ? kPageMostCut : kPageMostCut / 2, round = full / 2;
     *waves = U >= full || (U > round && (d > 64 || pages >= 8 || pages <= 2)) ? 1 : kStepWaves;
     int64_t S;
     if (*waves == 1) {

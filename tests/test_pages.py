@@ -69,6 +69,15 @@ def test_page_refusals_of_one_call():
     expect(binding.KF_EUNSUPPORTED, kf.new_page_workspace, fake(d=96), device="cpu")
 
 
+@pytest.mark.parametrize("L,B,H,G,d,max_pages", [(32, 1, 32, 1, 128, 64), (32, 4, 32, 1, 128, 64), (32, 8, 32, 1, 128, 64), (32, 8, 8, 4, 128, 64),
+                                                 (32, 1, 8, 4, 128, 512), (80, 1, 1, 8, 256, 4000), (28, 16, 3, 2, 64, 7), (2000, 1, 2, 1, 64, 300)])
+def test_a_workspace_serves_any_number_of_layers(L, B, H, G, d, max_pages):
+    """Fewer units take more splits each: the records of a layer can be more than those of all."""
+    of = dict(B=B, H=H, q_per_kv=G, d=d, max_pages=max_pages, pages=4096)
+    whole = kf.kf_page_workspace_bytes(fake(L=L, **of))
+    assert all(whole >= kf.kf_page_workspace_bytes(fake(L=l, **of)) > 0 for l in range(1, L))
+
+
 # ---------------------------------------------------------------- codes, written apart from any 8-bit type of torch
 MAGNITUDE = np.array([(c & 7) * 2.0 ** -9 if c < 8 else (8 + (c & 7)) * 2.0 ** ((c >> 3) - 10) for c in range(127)])
 VALUE = np.concatenate([MAGNITUDE, [math.nan], -MAGNITUDE, [math.nan]])
@@ -605,6 +614,33 @@ def test_layers_one_after_the_other_are_all_at_once():
             outs.append(out)
         runs.append((outs, [x.clone() for x in (c.K, c.V, c.k_scale, c.v_scale, c.table, c.len, c.refs)]))
     assert all(torch.equal(x, y) for x, y in zip(runs[0][0], runs[1][0])) and all(torch.equal(x, y) for x, y in zip(runs[0][1], runs[1][1]))
+
+
+@pytest.mark.gpu
+def test_a_layer_of_many_units_in_the_workspace_of_all_and_of_one():
+    """All layers are 1024 units of a split each, a layer 64 units of several: either in the other's workspace, where that serves it."""
+    L, B, H, d, n = 16, 1, 64, 128, 1000
+    c = kf.Pages.allocate(L, B, H, d, 16, 64, kf.BF16)
+    whole, one, g = kf.new_page_workspace(c), kf.new_page_workspace(c.layer(0)), torch.Generator().manual_seed(21)
+    k, v = (torch.randn((L, B, H, n, d), generator=g).bfloat16().cuda() for _ in range(2))
+    kf.kf_page_reserve(c, n, workspace=one)
+    kf.kf_page_write(c, k, v, n, workspace=one)
+    table = c.table[0, :16].cpu()
+    for i, ws in enumerate((whole, one)):
+        q, kn, vn = (torch.randn((L, B, H, d), generator=g).bfloat16() for _ in range(3))
+        heads = [(0, 0), (7, 33), (15, 63)]
+        held = [[(codes[l, table, h].view(torch.float8_e4m3fn).double() * by[l, table, h, None, None].double()).cpu() for codes, by in ((c.K, c.k_scale), (c.V, c.v_scale))]
+                for l, h in heads]
+        out = torch.zeros((L, B, H, d), device="cuda")
+        kf.kf_page_reserve(c, workspace=ws)
+        for l in range(L):
+            at = slice(l, l + 1)
+            kf.kf_page_step(c.layer(l), q[at].cuda(), kn[at].cuda(), vn[at].cuda(), d ** -0.5, out[at], workspace=ws)
+        for (l, h), (K, V) in zip(heads, held):
+            K, V = K.reshape(-1, d)[:n + i].numpy(), V.transpose(1, 2).reshape(-1, d)[:n + i].numpy()
+            want, tol = step_oracle(K, V, *(x[l, 0, h].double().numpy() for x in (q, kn, vn)), d ** -0.5, 0.0)
+            assert (np.abs(out[l, 0, h].double().cpu().numpy() - want) <= tol).all(), (i, l, h)
+    assert int(whole[:4].view(torch.int32)) == 0 == int(one[:4].view(torch.int32))
 
 
 @pytest.mark.gpu
