@@ -440,7 +440,7 @@ kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *sco
  * n and m bound a sequence's rows and keys; one whose rows lie outside [1, n] or whose keys lie outside [0, m] is left out.
  * Any q_per_kv is served.  out must not overlap the inputs.  The workspace (kf_prompt_workspace_bytes) needs no initial contents.
  * Errors: KF_EINVAL for sizes, null pointers, scale not finite, alignment (pointers and strides: 16 bytes), seq_n with q_start, seq_m
- * with k_start; KF_EUNSUPPORTED for a dtype / d pair that is not built, and for slopes beside a scale below 2^-60 in magnitude that is
+ * with k_start; KF_EUNSUPPORTED for a dtype / d pair that is not built, for launches of 2^32 threads and more, and for slopes beside a scale below 2^-60 in magnitude that is
  * not zero; KF_EWORKSPACE.
  */
 typedef struct {
@@ -473,6 +473,7 @@ kf_status kf_prompt_attend(const kf_prompt *p, const void *Q, const void *K, con
  * Pages are taken lowest number first, sequences in order.  table, len and refs serve all layers; a caller that runs its layers one
  * after the other passes the struct with L = 1 and the layer's K, V and scales to kf_page_write and kf_page_step.
  * dtype (KF_BF16 or KF_F16) is that of the rows that go in and of the queries.  d: 64, 128 or 256; q_per_kv: 1, 2, 4 or 8; B up to 8192.
+ * Calls whose launches would have 2^32 threads or more return KF_EUNSUPPORTED before the first of them.
  * The workspace is DEVICE memory, 16-byte aligned; only its first word must start as zero: it counts sequences, or pages of a unit, that a
  * kernel had to leave out.  What kf_page_workspace_bytes says of a struct serves every call on it and on any number of its layers; what it says of
  * one layer serves the steps of one layer, and the other calls on all of them.

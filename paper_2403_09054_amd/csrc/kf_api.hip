@@ -31,6 +31,8 @@ kf_status fail(kf_status st, const char* fmt, ...) {
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 constexpr int64_t kMaxGrid = 0x7fffffff;  // workgroups of a one-dimensional launch
+// Whether a launch of so many workgroups is one that the device takes: it counts a dimension's threads in 32 bits.
+bool fits(int64_t workgroups, int64_t threads) { return workgroups <= (int64_t)0xffffffff / threads; }
 // A fused step folds the merge of a split unit into the selection kernel (one workgroup per unit) only
 // while that workgroup walks the unit's tokens in a few strides; longer units take the merge launch,
 // which spreads a unit over several workgroups (32 heads x 9.8k tokens: 55.5 us folded, 52.6 us apart).
@@ -965,6 +967,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     const int64_t G = p->q_per_kv > 1 ? p->q_per_kv : 1, HQ = p->H * G, d = p->d;
     if (HQ > 1 << 24) return fail(KF_EINVAL, "too many heads");
     if (p->n * G > 1 << 30 || p->m > 1 << 30) return fail(KF_EINVAL, "too many rows (n=%d, q_per_kv=%d, m=%d)", p->n, p->q_per_kv, p->m);
+    if (!fits((int64_t)p->B * p->H, 256)) return fail(KF_EUNSUPPORTED, "%d sequences of %d heads exceed the largest launch", p->B, p->H);
     int64_t st[4][3];
     const int64_t* given[4] = {p->q_stride, p->k_stride, p->v_stride, p->out_stride};
     const int eb = p->dtype == KF_F32 ? 4 : 2;
@@ -1002,7 +1005,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     a->q_keep = p->scale == 0.0f ? 0u : ~0u;
     a->q_flip = p->scale < 0.0f ? (eb == 2 ? 0x80008000u : 0x80000000u) : 0u;
     kf::plan_attend(a, p->d, p->dtype);
-    if (a->blocks > kMaxGrid) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
+    if (!fits(a->blocks, a->threads)) return fail(KF_EUNSUPPORTED, "%d sequences of %d rows exceed the largest launch", p->B, p->n);
     *sums = align_up((size_t)a->ws_rows * a->S * p->d * 4, 256);
     // records and their references, parts, far tiles
     *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256) + align_up((size_t)a->ws_rows / a->block_rows * 4, 256) +
@@ -1137,7 +1140,7 @@ kf_status kf_page_write(const kf_pages* p, const void* k, const void* v, int32_t
     if (!k || !v) return fail(KF_EINVAL, "k and v must not be NULL");
     if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(KF_EINVAL, "k and v must be 16-byte aligned");
     if (n < 1 || (rows != 0 && rows < n)) return fail(KF_EINVAL, "n=%d must be positive and not above rows=%d", n, rows);
-    if ((int64_t)p->L * p->B * p->H * (((int64_t)n + 62) / 64 + 1) > kMaxGrid)
+    if (!fits((int64_t)p->L * p->B * p->H * (((int64_t)n + 62) / 64 + 1), kf::kPageThreads))
         return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads of %d rows exceed the largest launch", p->L, p->B, p->H, n);
     a.k = k;
     a.v = v;
@@ -1166,7 +1169,8 @@ kf_status kf_page_step(const kf_pages* p, const void* q, const void* k_new, cons
     a.seq_n = seq_n;
     a.sc = scale * kf::kLog2e;
     kf::plan_page_step(&a, U, p->d, m_hint ? m_hint : (int32_t)room);
-    if (U * a.S > kMaxGrid) return fail(KF_EUNSUPPORTED, "%lld units in %d splits each exceed the largest launch", (long long)U, a.S);
+    if (!fits(U * a.S, a.waves * kf::kWave) || (a.S > 1 && !fits(U * a.G, kf::kPageThreads)))  // splits, and the heads whose splits are joined
+        return fail(KF_EUNSUPPORTED, "%lld units of %d heads in %d splits each exceed the largest launch", (long long)U, a.G, a.S);
     a.ws_o = (float*)((char*)workspace + 256);
     a.ws_ml = (float2*)((char*)workspace + 256 + align_up((size_t)U * a.S * a.G * p->d * 4, 256));
     return end_pages(kf::launch_page_step(a, U, p->d, p->dtype, (hipStream_t)stream), "page step");
@@ -1198,7 +1202,7 @@ kf_status kf_page_compact(const kf_pages* p, const int32_t* keep, int32_t k, con
     if (!keep) return fail(KF_EINVAL, "keep is NULL");
     const int64_t room = (int64_t)p->max_pages * KF_PAGE_TOKENS;
     if (k < 1 || k > room) return fail(KF_EINVAL, "k=%d outside [1, %lld]", k, (long long)room);
-    if ((int64_t)p->L * p->B * p->H * ((k + 63) / 64) > kMaxGrid - 8)
+    if (!fits((int64_t)p->L * p->B * p->H * ((k + 63) / 64), kf::kPageThreads))
         return fail(KF_EUNSUPPORTED, "%d layers of %d sequences and %d heads of %d tokens exceed the largest launch", p->L, p->B, p->H, k);
     a.keep = keep;
     a.kept = k;

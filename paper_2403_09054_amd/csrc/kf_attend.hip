@@ -600,6 +600,7 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
     else if (!wide && a->m > 512 && rows <= 32 && units <= 64) a->shape = kAttendFew;
     else if (!wide && a->m > 512 && b64 > 64 && b64 <= 256) a->shape = kAttendOne;
     a->block_rows = a->shape == kAttendMany ? 128 : a->shape == kAttendFew ? 32 : 64;
+    a->threads = a->shape == kAttendOne ? 512 : 256;
     a->tiles = (int32_t)((rows + a->block_rows - 1) / a->block_rows);
     a->S = 1;
     const int64_t blocks = units * a->tiles;

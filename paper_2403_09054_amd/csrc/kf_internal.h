@@ -322,7 +322,7 @@ struct AttendArgs {
     int32_t B, n, m, H, G;
     float sc;                // |scale| * log2(e); the queries take the scale's sign, or zero with it
     uint32_t q_keep, q_flip;
-    int32_t shape, block_rows;  // of a workgroup: many rows, fewer, a few
+    int32_t shape, block_rows, threads;  // of a workgroup: many rows, fewer, a few
     int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys at most
     int32_t chunk;           // keys that each of them walks
     int32_t spread;          // XCDs that a cached head's blocks are dealt out to
@@ -337,6 +337,7 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype);
 hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream);
 
 // ------------------------------------------------------------------ pages of an 8-bit cache (kf_pages.hip)
+constexpr int32_t kPageThreads = 256;   // of a workgroup, but for the step's of one wave and those that work on the table
 constexpr int32_t kPageMaxRows = 8192;  // sequences: the table's launches hold a word of each in LDS
 struct PageArgs {
     uint8_t* K;              // [L][pages][H][64][d]

@@ -24,7 +24,6 @@
 
 namespace kf {
 
-constexpr int kPageThreads = 256;
 constexpr int kPageWaves = kPageThreads / kWave;
 constexpr int kStepWaves = 4;        // of a workgroup of the step, or one
 constexpr int kTableThreads = 1024;

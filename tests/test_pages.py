@@ -69,6 +69,16 @@ def test_page_refusals_of_one_call():
     expect(binding.KF_EUNSUPPORTED, kf.new_page_workspace, fake(d=96), device="cpu")
 
 
+def test_launches_of_2_to_the_32_threads_are_refused():
+    """Before any launch of the call: the step's own is smaller than the one that joins its splits, for each head of a unit."""
+    units = dict(L=1 << 9, B=1 << 9, H=1 << 6)
+    expect(binding.KF_EUNSUPPORTED, CALLS["write"], fake(**units), n=1)
+    expect(binding.KF_EUNSUPPORTED, CALLS["compact"], fake(**units), k=64)
+    expect(binding.KF_EUNSUPPORTED, CALLS["step"], fake(max_pages=1000, **units))
+    expect(binding.KF_EUNSUPPORTED, CALLS["step"], fake(L=80, B=8192, H=8, q_per_kv=8, max_pages=65))
+    expect(binding.KF_EUNSUPPORTED, CALLS["write"], fake(L=1, B=1, H=1), n=(1 << 31) - 1)
+
+
 @pytest.mark.parametrize("L,B,H,G,d,max_pages", [(32, 1, 32, 1, 128, 64), (32, 4, 32, 1, 128, 64), (32, 8, 32, 1, 128, 64), (32, 8, 8, 4, 128, 64),
                                                  (32, 1, 8, 4, 128, 512), (80, 1, 1, 8, 256, 4000), (28, 16, 3, 2, 64, 7), (2000, 1, 2, 1, 64, 300)])
 def test_a_workspace_serves_any_number_of_layers(L, B, H, G, d, max_pages):

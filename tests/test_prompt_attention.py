@@ -43,6 +43,13 @@ def test_prompt_refusals():
     assert kf.kf_prompt_workspace_bytes(kf.Prompt(1, 1, 8000, 2, 128, kf.BF16, 1.0)) > kf.kf_prompt_workspace_bytes(kf.Prompt(64, 4096, 4096, 32, 128, kf.BF16, 1.0)) > 0
 
 
+def test_launches_of_2_to_the_32_threads_are_refused():
+    of = dict(n=1, m=1, d=128, dtype=kf.BF16, scale=1.0)
+    assert kf.kf_prompt_workspace_bytes(kf.Prompt(B=4095, H=4097, **of)) > 0 == kf.kf_prompt_workspace_bytes(kf.Prompt(B=4096, H=4096, **of))
+    for big in (dict(B=4096, H=4096), dict(B=1 << 12, H=1 << 9, n=1024), dict(B=(1 << 31) - 1, H=(1 << 24) - 1, n=1 << 30)):
+        expect(binding.KF_EUNSUPPORTED, kf.kf_prompt_attend, kf.Prompt(**{**of, **big}), 0x1000, 0x2000, 0x3000, 0x4000, workspace=(0x100000, 1 << 40), stream=0)
+
+
 # ---------------------------------------------------------------- the definition
 def attend_oracle(q, k, v, scale, slope, dt):
     """One head: [nq, d], [nk, d] -> its rows, and how far a row may be off.
