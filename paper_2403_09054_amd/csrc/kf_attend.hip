@@ -628,23 +628,27 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
 }
 
 template <typename T, int D, typename SHAPE>
-static void launch_attend_s(const AttendArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)a.blocks), block(SHAPE::WR * SHAPE::WK * kWave);
+static hipError_t launch_attend_s(const AttendArgs& a, hipStream_t st) {
+    // tiles, records and the grid were sized for these
+    if (a.block_rows != SHAPE::WR * 32 || a.threads != SHAPE::WR * SHAPE::WK * kWave) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)a.blocks), block((unsigned)a.threads);
+    if (a.far_tiles)
+        hipLaunchKernelGGL((attend_norms_kernel<T, D>), dim3((unsigned)a.far_tiles, (unsigned)(a.B * a.H)), dim3(256), 0, st, a);
     if (a.slopes) hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((attend_kernel<T, D, SHAPE, false>), grid, block, 0, st, a);
+    if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * a.block_rows);
+    return hipGetLastError();
 }
 template <typename T, int D>
 static hipError_t launch_attend_d(const AttendArgs& a, hipStream_t st) {
     using S = AttendShapes<D * (int)sizeof(T)>;
-    if (a.far_tiles)
-        hipLaunchKernelGGL((attend_norms_kernel<T, D>), dim3((unsigned)a.far_tiles, (unsigned)(a.B * a.H)), dim3(256), 0, st, a);
-    if (a.shape == kAttendMany) launch_attend_s<T, D, typename S::Many>(a, st);
-    else if constexpr (D * sizeof(T) > 256) launch_attend_s<T, D, typename S::Fewer>(a, st);
-    else if (a.shape == kAttendFewer) launch_attend_s<T, D, typename S::Fewer>(a, st);
-    else if (a.shape == kAttendOne) launch_attend_s<T, D, typename S::One>(a, st);
-    else launch_attend_s<T, D, typename S::Few>(a, st);
-    if (a.S > 1) hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.ws_rows / 4)), dim3(256), 0, st, a, a.tiles * a.block_rows);
-    return hipGetLastError();
+    if (a.shape == kAttendMany) return launch_attend_s<T, D, typename S::Many>(a, st);
+    if (a.shape == kAttendFewer) return launch_attend_s<T, D, typename S::Fewer>(a, st);
+    if constexpr (D * sizeof(T) <= 256) {
+        if (a.shape == kAttendOne) return launch_attend_s<T, D, typename S::One>(a, st);
+        if (a.shape == kAttendFew) return launch_attend_s<T, D, typename S::Few>(a, st);
+    }
+    return hipErrorInvalidValue;                 // wide rows have no such shape
 }
 
 hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream) {

@@ -43,6 +43,41 @@ def test_prompt_refusals():
     assert kf.kf_prompt_workspace_bytes(kf.Prompt(1, 1, 8000, 2, 128, kf.BF16, 1.0)) > kf.kf_prompt_workspace_bytes(kf.Prompt(64, 4096, 4096, 32, 128, kf.BF16, 1.0)) > 0
 
 
+SHAPES = r"""
+#include "kf_internal.h"
+#include <cstdio>
+int main() {  // shapes that the plan did not size its tiles and records for: refused, and nothing is launched
+    const int type[][2] = {{KF_F32, 64}, {KF_F32, 128}, {KF_BF16, 64}, {KF_BF16, 128}, {KF_BF16, 256}, {KF_F16, 64}, {KF_F16, 256}};
+    int calls = 0;
+    for (auto& t : type)
+        for (int n : {1, 100, 3000})
+            for (int units : {1, 40, 700})
+                for (int shape = 0; shape < 5; ++shape) {
+                    kf::AttendArgs a = {};
+                    a.B = units, a.H = 1, a.G = 1, a.n = n, a.m = 3000;
+                    kf::plan_attend(&a, t[1], t[0]);
+                    if (shape == a.shape) continue;
+                    a.shape = shape;
+                    if (kf::launch_attend(a, t[1], t[0], nullptr) != hipErrorInvalidValue) return printf("%d x %d, %d rows of %d: shape %d\n", t[0], t[1], n, units, shape), 1;
+                    ++calls;
+                }
+    return calls > 200 ? 0 : 1;
+}
+"""
+
+
+def test_a_shape_that_was_not_planned_is_refused(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(kf.lib_path())
+    source, program = tmp_path / "shapes.hip", tmp_path / "shapes"
+    source.write_text(SHAPES)
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "--offload-arch=gfx950", "-std=c++17", "-I", os.path.join(root, "csrc"), str(source), "-o", str(program),
+                    "-L", root, "-lkeyformer", f"-Wl,-rpath,{root}"], check=True, timeout=100)
+    r = subprocess.run([str(program)], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
 def test_launches_of_2_to_the_32_threads_are_refused():
     of = dict(n=1, m=1, d=128, dtype=kf.BF16, scale=1.0)
     assert kf.kf_prompt_workspace_bytes(kf.Prompt(B=4095, H=4097, **of)) > 0 == kf.kf_prompt_workspace_bytes(kf.Prompt(B=4096, H=4096, **of))
