@@ -211,6 +211,74 @@ def test_attention_matches_the_definition(case):
     assert bool((out == 7.0).all())  # nothing else was written
 
 
+MANY = [  # workgroups of 128 rows; heads that are a multiple of the XCDs and heads that are none
+    (64, 130, 130, 16, 1, 128, kf.BF16, False, "padded"),
+    (64, 130, 130, 16, 1, 128, kf.F16, True, "plain"),
+    (64, 129, 140, 16, 1, 64, kf.BF16, True, "padded"),
+    (64, 130, 130, 16, 1, 64, kf.F16, False, "packed"),
+    (64, 130, 130, 16, 1, 64, kf.F32, True, "cache"),
+    (32, 130, 130, 16, 1, 256, kf.BF16, True, "packed"),
+    (32, 140, 200, 16, 1, 256, kf.F16, False, "padded"),
+    (32, 70, 97, 8, 4, 128, kf.F32, False, "padded"),     # three blocks of 128 rows of four heads each, cut through a position
+    (39, 70, 70, 9, 5, 64, kf.BF16, False, "packed"),
+    (8, 2100, 2100, 8, 1, 128, kf.BF16, True, "plain"),   # far keys are looked for
+    (5, 2100, 2111, 7, 2, 64, kf.F16, True, "padded"),    # blocks of a head dealt out over XCDs
+    (5, 4100, 4100, 7, 1, 128, kf.BF16, False, "packed"),
+]
+
+
+def takes_128_rows(p):
+    """The rule by which a call does."""
+    return p.B * p.H * -(-p.n * p.q_per_kv // 128) >= (512 if p.d * (4 if p.dtype == kf.F32 else 2) > 256 else 1024)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "x".join(map(str, c)))
+def test_workgroups_of_128_rows_match_the_definition(case):
+    p, (Q, K, V, out), views, slopes, dt = make(case)
+    assert takes_128_rows(p)
+    kf.kf_prompt_attend(p, Q, K, V, out, workspace=kf.new_prompt_workspace(p))
+    torch.cuda.synchronize()
+    assert not bool((torch.cat([o.reshape(-1) for *_, o in views]).reshape(-1, p.d) == 7.0).all(1).any())  # every row was written
+    for b, (q, k, v, o) in enumerate(views):
+        G = p.q_per_kv
+        for h in range(p.H) if p.n < 1000 else ((b + 3) % p.H,) if b < 3 or b == p.B - 1 else ():
+            at = slice(h * G, h * G + G)
+            want, tol = oracle(q[at].cpu(), k[h:h + 1].cpu(), v[h:h + 1].cpu(), p.scale, None if slopes is None else slopes[at], G, dt)
+            near(o[at], want, tol, (case, b, h))
+        o.fill_(7.0)
+    assert bool((out == 7.0).all())  # nothing else was
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,dtype,d", [(64, kf.BF16, 128), (64, kf.F16, 64), (32, kf.BF16, 256), (32, kf.F32, 128)])
+def test_what_rows_of_a_workgroup_of_128_do_not_see_does_not_reach_them(B, dtype, d):
+    n, m = 150, 190
+    p, (Q, K, V, out), views, _, dt = make((B, n, m, 16, 1, d, dtype, False, "plain"))
+    assert takes_128_rows(p)
+    ws = kf.new_prompt_workspace(p)
+    kf.kf_prompt_attend(p, Q, K, V, out, workspace=ws)
+    clean = out.clone()
+    for j in (0, m - n, m - n + 1, 90, 127, 128, m - 2, m - 1):
+        first = max(0, j - (m - n))
+        for tensor, value in ((V, math.nan), (V, math.inf), (K, math.nan)):
+            keep = tensor[7, 5, j].clone()
+            tensor[7, 5, j, 9] = value
+            out.fill_(7.0)
+            kf.kf_prompt_attend(p, Q, K, V, out, workspace=ws)
+            tensor[7, 5, j] = keep
+            got, was = out[7, :, 5].clone(), clean[7, :, 5]
+            out[7, :, 5] = was
+            assert torch.equal(out, clean)
+            # a row that does not see it: sums as they were, but for the terms' order (their 2 * (m + 64) U of at most |v| = 6)
+            near(got[:first], was[:first].double().cpu(), torch.finfo(dt).eps * was[:first].double().cpu().abs() + 12 * (m + 64) * U, (j, value))
+            seen = got[first:].float()
+            if tensor is K:
+                assert bool(torch.isnan(seen).all())
+            else:
+                assert not bool(torch.isfinite(seen[:, 9]).any()) and bool(torch.isfinite(torch.cat([seen[:, :9], seen[:, 10:]], 1)).all())
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.0, -0.125, 40.0])
 def test_scales_of_any_sign_and_size(scale):
@@ -385,6 +453,23 @@ def test_far_rows_pass_32_bits():
 def test_far_rows_pass_32_bits_inside_a_tile():
     """Tiles of 128 keys whose tokens lie 2^27 bytes apart, shared by workgroups of eight waves."""
     H, n, m, d, step = 40, 128, 130, 64, 1 << 26
+    flat = torch.empty(step * (m - 1) + 2 * H * d, dtype=torch.bfloat16, device="cuda")
+    K, V = (torch.as_strided(flat, (1, H, m, d), (0, d, step, 1), i * H * d) for i in range(2))
+    g = torch.Generator().manual_seed(2)
+    for x in (K, V):
+        x.copy_(torch.randn((1, H, m, d), generator=g).bfloat16())
+    Q = torch.randn((1, H, n, d), generator=g).bfloat16().cuda()
+    out = torch.zeros((1, n, H, d), dtype=torch.bfloat16, device="cuda")
+    p = kf.Prompt(1, n, m, H, d, kf.BF16, 0.1, k_stride=(0, d, step), v_stride=(0, d, step))
+    kf.kf_prompt_attend(p, Q, K, V, out, workspace=kf.new_prompt_workspace(p))
+    want, tol = oracle(Q[0].cpu(), K[0].cpu(), V[0].cpu(), 0.1, None, 1, torch.bfloat16)
+    near(out[0].transpose(0, 1), want, tol, "far")
+
+
+@pytest.mark.gpu
+def test_far_rows_pass_32_bits_inside_a_tile_of_eight_waves():
+    """More than 512 keys, 2^27 bytes apart, and 65 to 256 workgroups: eight waves bring 64 rows of a tile of 128 at once."""
+    H, n, m, d, step = 80, 9, 520, 64, 1 << 26
     flat = torch.empty(step * (m - 1) + 2 * H * d, dtype=torch.bfloat16, device="cuda")
     K, V = (torch.as_strided(flat, (1, H, m, d), (0, d, step, 1), i * H * d) for i in range(2))
     g = torch.Generator().manual_seed(2)
