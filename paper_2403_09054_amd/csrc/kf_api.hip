@@ -1009,7 +1009,7 @@ static kf_status check_prompt(const kf_prompt* p, kf::AttendArgs* a, size_t* sum
     *sums = align_up((size_t)a->ws_rows * a->S * p->d * 4, 256);
     // records and their references, parts, far tiles
     *bytes = 256 + *sums + align_up((size_t)a->ws_rows * a->S * sizeof(float2), 256) + align_up((size_t)a->ws_rows / a->block_rows * 4, 256) +
-             align_up((size_t)a->far_tiles * p->B * p->H * 4, 256);
+             align_up((size_t)a->far_tiles * p->B * p->H * sizeof(float2), 256);
     return KF_OK;
 }
 
@@ -1038,7 +1038,7 @@ kf_status kf_prompt_attend(const kf_prompt* p, const void* Q, const void* K, con
     char* w = (char*)workspace + 256 + sums + align_up((size_t)a.ws_rows * a.S * sizeof(float2), 256);
     a.ws_parts = (int32_t*)w;
     w += align_up((size_t)a.ws_rows / a.block_rows * 4, 256);
-    a.ws_kn = a.far_tiles ? (float*)w : nullptr;
+    a.ws_kn = a.far_tiles ? (float2*)w : nullptr;
     const hipError_t e = kf::launch_attend(a, p->d, p->dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(KF_EDEVICE, "prompt attention launch: %s", hipGetErrorString(e));
     g_err[0] = 0;

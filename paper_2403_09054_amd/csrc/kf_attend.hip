@@ -12,7 +12,7 @@
 //
 // What bounds it: many rows, the matrix cores beside the vector unit (128 elements a row: 512 operations of the one for each exponential,
 // sum and rounding of the other), and the power they draw.  8 x 32 heads x 4096 x 128 bf16, causal: 1180 us, 930 TFLOP/s (a product of
-// 8192^3: 1155 to 1394); with a position bias, far tiles left out, 830; 8 heads of 8 x 512 rows at the end of 8192 keys 500 us, 1070 TFLOP/s; 256
+// 8192^3: 1155 to 1394); with a position bias, far tiles left out, 887; 8 heads of 8 x 512 rows at the end of 8192 keys 500 us, 1070 TFLOP/s; 256
 // elements 760, 64 elements 760, fp32 59 (its own products' rate).  Counters: no bank conflicts in LDS, matrix cores busy 40 % of the cycles at 2.0
 // GHz; inputs of zeros run 10 % faster.  Few rows: the chain of a walk, 8 us for 1000 keys, and the join; 16 x 2048 x 128 40 us.
 //
@@ -73,6 +73,22 @@ __device__ __forceinline__ bool clean_piece(u32x4_t& v) {
     return bad;
 }
 
+// Magnitudes in the order of their bits: the largest or the least (of two 16-bit ones in a word, in either half), and the number.
+template <typename T, bool LEAST>
+__device__ __forceinline__ uint32_t piece_magnitude(const u32x4_t& v, uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = sizeof(T) == 4 ? v[i] & 0x7FFFFFFFu : v[i] & 0x7FFFu, hi = sizeof(T) == 4 ? lo : v[i] >> 16 & 0x7FFFu;
+        m = LEAST ? min(m, min(lo, hi)) : max(m, max(lo, hi));
+    }
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ float magnitude(uint32_t m) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+    else return __is_same(T, bf16_t) ? __uint_as_float(m << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)m);
+}
+
 // Largest of a lane's and its partner's in the wave's other half.
 __device__ __forceinline__ float half_max(float v) {
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -83,8 +99,10 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
-constexpr int kFarTile = 128;        // keys whose largest norm is kept
-constexpr float kAttendFar = 40.0f;  // 65536 keys that are left out weigh less than 2^-24 of a row together
+constexpr int kFarTile = 128;         // keys whose largest norm and value are kept
+// Keys are left out where all of them together have less than 2^-25 of what a row's own key has of each element, and of its weight; or
+// where each weighs less than 2^-150 of the row's own key, which is nothing in 32 bits.
+constexpr float kAttendFar = 25.0f, kAttendNothing = 150.0f;
 // A reference is raised once a row's largest exponent is this far above the place where raising puts it.
 constexpr float kAttendSlack = 8.0f;
 // Raising puts a row's reference this far below its largest exponent.  In half precision terms then reach from 2^15 down to 2^-24, so that
@@ -169,38 +187,47 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
     const int kend = min(nk, off + min(R0 + ROWS - 1, rows - 1) / a.G + 1);
     int t0 = 0, t1 = kend > 0 ? (kend + BK - 1) / BK : 0;
     if constexpr (BIAS) {
-        // Far keys that cannot matter.  A row's largest logit is at least its own key's; one at distance D is at most sc |q| |k| - slope D:
-        // where that lies kAttendFar below for every row, a tile of keys is left out, with all before it.  (A tile that holds a value which
-        // is no number, or infinite, has an infinite norm; what is no number makes no row's bound hold, nor does a bias that rises.)
+        // Far keys that cannot matter.  The logit of one at distance D is at most sc |q| |k| - slope D: where that lies so far below the own
+        // key's of every row, as the number of keys, the tile's largest value and the least element of the row's own value ask for, a tile of
+        // keys is left out, with all before it.  (A tile that holds a value which is no number, or infinite, has an infinite norm; what is no
+        // number makes no row's bound hold, nor does a bias that rises.)
         if (a.ws_kn && t1 > 0) {
             float qq = 0.0f, own = 0.0f;
-            const char* mine = Kh + (int64_t)min(max(pos, 0), nk - 1) * krow + half * 16;
-            u32x4_t k[KS];
+            const int64_t mine = min(max(pos, 0), nk - 1);
+            u32x4_t k[KS], v[KS];
+            uint32_t least = ~0u;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) k[s] = *(const u32x4_t*)(mine + s * 32);
+            for (int s = 0; s < KS; ++s) {
+                k[s] = *(const u32x4_t*)(Kh + mine * krow + half * 16 + s * 32);
+                v[s] = *(const u32x4_t*)(Vh + mine * vrow + half * 16 + s * 32);
+            }
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 qq = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, q[s]), qq);
                 own = dot_piece<T>(__builtin_bit_cast(uint4, q[s]), __builtin_bit_cast(uint4, k[s]), own);
+                least = piece_magnitude<T, true>(v[s], least);
             }
             qq = half_sum(qq);
             own = half_sum(own);
             const bool odd = __any(!(qq < INFINITY) || !(fabsf(own) < INFINITY) || slope < 0.0f);
+            own *= -a.sc;
+            const float value = own - hw_log2(-half_max(-magnitude<T>(least)));
             qq = odd ? INFINITY : wave_max(qq);
-            own = wave_max(-own);
-            const float flat = -wave_max(-slope);
-            if (lane == 0) far_s[wv] = make_float4(qq, flat, own, 0.0f);
+            const float flat = -wave_max(-slope), most = wave_max(own), most_value = wave_max(value);
+            if (lane == 0) far_s[wv] = make_float4(qq, flat, most, most_value);
             __syncthreads();
             float4 all = far_s[0];
 #pragma unroll
-            for (int w = 1; w < W; ++w) all.x = fmaxf(all.x, far_s[w].x), all.y = fminf(all.y, far_s[w].y), all.z = fmaxf(all.z, far_s[w].z);
+            for (int w = 1; w < W; ++w) all.x = fmaxf(all.x, far_s[w].x), all.y = fminf(all.y, far_s[w].y), all.z = fmaxf(all.z, far_s[w].z), all.w = fmaxf(all.w, far_s[w].w);
             const int lowest = off + R0 / a.G, count = (a.m + kFarTile - 1) / kFarTile;
-            const float* kn = a.ws_kn + (int64_t)unit * count;
-            const float qn = sqrtf(all.x);
+            const float2* kn = a.ws_kn + (int64_t)unit * count;
+            const float qn = sqrtf(all.x), need = kAttendFar + hw_log2((float)max(lowest, 1));
             int from = lowest > 0 ? lowest / kFarTile : 0;  // tiles that end before the lowest row
             for (int i = 0; i < from; i += kWave) {
                 const int tile = i + lane;
-                const bool far = tile < from && a.sc * (qn * kn[min(tile, from - 1)] + all.z - all.y * (float)(lowest - (tile * kFarTile + kFarTile - 1))) < -kAttendFar;
+                const float2 t = kn[min(tile, from - 1)];
+                const float below = fminf(need + fmaxf(all.w + hw_log2(t.y), all.z), kAttendNothing + all.z);
+                const bool far = tile < from && a.sc * (qn * t.x - all.y * (float)(lowest - (tile * kFarTile + kFarTile - 1))) < -below;
                 const uint64_t no = __ballot(!far);
                 if (no) {
                     from = min(from, i + __builtin_ctzll(no));
@@ -487,7 +514,7 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
         }
 }
 
-// Largest norm of kFarTile keys, or infinity where a key or a value among them is infinite or no number: blockIdx = (tile, unit).
+// Largest norm of kFarTile keys, or infinity where a key or a value among them is infinite or no number, and largest value: blockIdx = (tile, unit).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_norms_kernel(const AttendArgs a) {
     constexpr int CH = D * (int)sizeof(T) / 16, RPX = 256 / CH;
@@ -511,6 +538,7 @@ __global__ void __launch_bounds__(256) attend_norms_kernel(const AttendArgs a) {
         }
     }
     float most = 0.0f;
+    uint32_t value = 0;
 #pragma unroll
     for (int x = 0; x < kFarTile / RPX; ++x) {
         float d = dot_piece<T>(k[x], k[x], 0.0f);
@@ -518,9 +546,11 @@ __global__ void __launch_bounds__(256) attend_norms_kernel(const AttendArgs a) {
         for (int o = 1; o < CH; o <<= 1) d += __shfl_xor(d, o, kWave);
         u32x4_t w = {v[x].x, v[x].y, v[x].z, v[x].w};
         most = fmaxf(most, clean_piece<T>(w) || !(d < INFINITY) ? INFINITY : d);
+        value = piece_magnitude<T, false>(w, value);
     }
     most = block_max<256>(most, red);
-    if (tid == 0) a.ws_kn[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sqrtf(most);
+    const float large = block_max<256>(magnitude<T>(value), red);
+    if (tid == 0) a.ws_kn[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = make_float2(sqrtf(most), large);
 }
 
 // Joins the parts of a row: one wave a row, a lane takes D / 64 elements.
@@ -620,9 +650,9 @@ void plan_attend(AttendArgs* a, int32_t d, int32_t dtype) {
     while (units * a->spread % kXcds) a->spread *= 2;
     if (a->H % kXcds == 0 || a->tiles < 4 * a->spread) a->spread = 1;
     a->blocks = units * a->spread * ((a->tiles + a->spread - 1) / a->spread) * a->S;  // of the launch
-    // A row of far tiles is looked for where a key is read often enough: the search is a launch that reads K and V once more, 95 of 835 us of
-    // 8 x 32 x 4096 x 128, which take 1350 without.  4 x 32 x 4096 430 and 665 us, 32 x 2048 57 and 67, 8 x 4096 72 and 70, 8 x 2048 37 and 32 (few
-    // workgroups, which wait for the head of the gentlest slope); 8 x 32 x 1024 136 with it and 132.
+    // A row of far tiles is looked for where a key is read often enough: the search is a launch that reads K and V once more, 95 of 887 us of
+    // 8 x 32 x 4096 x 128, which take 1350 without.  4 x 32 x 4096 450 and 665 us, 32 x 2048 62 and 67, 8 x 4096 73 and 70, 8 x 2048 40 and 32 (few
+    // workgroups, which wait for the head of the gentlest slope); 8 x 32 x 1024 137 with it and 132.
     a->far_tiles = a->slopes && (int64_t)a->n * a->G >= 2048 && units <= 65535 ? (a->m + kFarTile - 1) / kFarTile : 0;
     a->ws_rows = a->S > 1 ? blocks * a->block_rows : 0;
 }

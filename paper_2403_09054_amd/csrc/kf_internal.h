@@ -326,12 +326,12 @@ struct AttendArgs {
     int32_t tiles, S;        // row blocks of a cached head, workgroups that share a block's walk over the keys at most
     int32_t chunk;           // keys that each of them walks
     int32_t spread;          // XCDs that a cached head's blocks are dealt out to
-    int32_t far_tiles;       // of a cached head, whose norms tell what a position bias rules out; 0: not looked for
+    int32_t far_tiles;       // of a cached head, whose norms and values tell what a position bias rules out; 0: not looked for
     int64_t blocks, ws_rows; // workgroups; rows of a split launch's records, padded
     float* ws_o;             // [ws_rows][S][d]
     float2* ws_ml;           // [ws_rows][S] reference and sum
     int32_t* ws_parts;       // [B*H][tiles] how many share a block's walk
-    float* ws_kn;            // [B*H][far_tiles], or NULL
+    float2* ws_kn;           // [B*H][far_tiles] largest norm of a key, largest element of a value; or NULL
 };
 void plan_attend(AttendArgs* a, int32_t d, int32_t dtype);
 hipError_t launch_attend(const AttendArgs& a, int32_t d, int32_t dtype, hipStream_t stream);

@@ -365,6 +365,26 @@ def test_far_keys_are_left_out_only_where_they_cannot_matter(dtype, d, H, G, n, 
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,n,m,big", [(kf.F32, 64, 2304, 2304, 1e20), (kf.BF16, 128, 2304, 2304, 2.0 ** 34), (kf.BF16, 64, 2100, 2500, 1e30), (kf.F16, 64, 2304, 2304, 6e4)])
+def test_far_values_that_are_large_and_elements_that_only_far_keys_have(dtype, d, n, m, big):
+    """What a far key weighs times what it holds: finite values some powers of ten above their neighbours', and neighbours of zeros."""
+    dt, g = TYPES[dtype], torch.Generator().manual_seed(m)
+    Q, K, V = (torch.randn((1, r, d), generator=g).to(dt) for r in (n, m, m))
+    V[0, 64:, 1] = 0.0
+    V[0, 1500:1600] = 0.0                       # rows whose own key holds nothing
+    alone = V.clone()
+    for at in (5, 700):
+        V[0, at] = (V[0, at].float() * 0.2 * big).to(dt)
+    p = kf.Prompt(1, n, m, 1, d, dtype, 0.02, slopes=torch.tensor([0.02]).cuda())
+    ws = kf.new_prompt_workspace(p)
+    for v in (V, alone):
+        out = torch.zeros((1, n, 1, d), dtype=dt, device="cuda")
+        kf.kf_prompt_attend(p, Q[None].cuda(), K[None].cuda(), v[None].cuda(), out, workspace=ws)
+        want, tol = oracle(Q, K, v, 0.02, torch.tensor([0.02]), 1, dt)
+        near(out[0].transpose(0, 1), want, tol, "far values")
+
+
+@pytest.mark.gpu
 def test_far_keys_that_a_rising_bias_prefers():
     """The far end of a far tile has more of a negative slope than its near end: every row's first key outweighs its own."""
     n, d, slope, g = 2304, 128, -10.0, torch.Generator().manual_seed(3)
