@@ -501,6 +501,10 @@ __global__ void __launch_bounds__(SHAPE::WR * SHAPE::WK * kWave, (D * (int)sizeo
                 *(float4*)(w + i * 32 + y * 8 + half * 4) = make_float4(o[i][4 * y], o[i][4 * y + 1], o[i][4 * y + 2], o[i][4 * y + 3]);
         return;
     }
+    if (l == 0.0f) {                             // nothing but logits at minus infinity, whatever their values hold
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = (f32x16)(0.0f);
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     char* w = (char*)a.out + ((a.q_start ? q0 * a.o_st : b * a.o_sb) + qh * a.o_sh + qi * a.o_st) * EB;
 #pragma unroll
@@ -594,6 +598,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
         }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = l == 0.0f ? 0.0f : x[e];
     T* w = (T*)a.out + (a.q_start ? q0 * a.o_st : b * a.o_sb) + qh * a.o_sh + qi * a.o_st + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) {

@@ -454,6 +454,24 @@ def test_keys_at_minus_infinity_and_sequences_that_are_none():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,m", [(40, 40), (40, 600), (3, 3000), (2, 130)])
+def test_rows_at_minus_infinity_are_zero_whatever_their_values_hold(n, m):
+    """Rows that see keys, all of them at minus infinity: walked whole, by waves that share them, and in parts."""
+    d = 64
+    Q = torch.ones((1, 1, n, d), dtype=torch.bfloat16, device="cuda")
+    K, V = torch.zeros((1, 1, m, d), dtype=torch.bfloat16, device="cuda"), torch.ones((1, 1, m, d), dtype=torch.bfloat16, device="cuda")
+    K[..., 0] = -math.inf
+    K[0, 0, -1, 0] = 0.0                         # the last row sees one that is not
+    V[0, 0, ::3, 5], V[0, 0, 1::3, 6] = math.inf, math.nan
+    V[0, 0, -1] = 3.0
+    out = torch.full((1, n, 1, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    p = kf.Prompt(1, n, m, 1, d, kf.BF16, 1.0)
+    kf.kf_prompt_attend(p, Q, K, V, out, workspace=kf.new_prompt_workspace(p))
+    assert bool((out[0, :-1] == 0).all())
+    assert bool((out[0, -1, 0, :5] == 3.0).all()) and bool((out[0, -1, 0, 7:] == 3.0).all())
+
+
+@pytest.mark.gpu
 def test_far_rows_pass_32_bits():
     """Keys whose byte offsets lie beyond 2^32: a head's rows far apart."""
     d, m, step = 128, 40, 1 << 26  # elements between tokens
