@@ -33,10 +33,10 @@ typedef __attribute__((address_space(3))) char lds_char;
 // 16 bytes a lane from memory to LDS, at `lds` (the wave's) + 16 * lane.  The compiler does not know of them: whoever reads them waits for
 // vmcnt(0) and the workgroup first.  (Its own form of this waits for all of them ahead of any read of LDS.)
 __device__ __forceinline__ void to_lds(uint32_t lds, const char* base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void to_lds(uint32_t lds, const char* p) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
 }
 
 // What a workgroup does: WR waves of 32 rows, times WK waves that share each tile's keys; SB blocks of 32 keys are a step of a wave, NB are
