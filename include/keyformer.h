@@ -430,8 +430,10 @@ kf_status kf_beam_select(const kf_beams *b, const void *logits, const float *sco
  * over the sequence's nk keys: a whole prompt (nk = nq), or the last rows of one whose earlier keys are there.  A row that sees no
  * key (nq > nk), or whose logits are all minus infinity, is zero.  What a row does not see does not reach it, whatever it holds.
  * Logits, softmax and sums have 32 bits; with 16-bit elements the probabilities are rounded to the element type for their
- * product with V.  A row of out is rounded once.  With a position bias, keys far before a row are not walked where all of them together
- * have less than 2^-25 of what the row's own key has, of the weight and of each element of out; or where each weighs less than 2^-150 of it.
+ * product with V (the sum that divides a row is that of the unrounded ones), those of half precision below 2^-31 of a row's largest to zero, and
+ * the bias is where a logit's sum begins, which is rounded at the larger of the two.  A row of out is rounded once.  With a position
+ * bias, keys far before a row are not walked where all of them together have less than 2^-25 of what the row's own key has, of the weight and of
+ * each element of out; or where each weighs less than 2^-150 of it.
  *   strides : elements between sequences, heads, tokens; all three zero: Q [B][H*q_per_kv][n][d], K and V [B][H][m][d] (a layer of a
  *             cache with cap = m), out [B][n][H*q_per_kv][d]; of packed rows: [tokens][heads][d].  Tokens of K and V lie at most 2^27 bytes apart.
  *   q_start, k_start : DEVICE [B+1] or NULL.  Packed sequences: b's rows are tokens start[b] .. start[b+1]-1 of one list (the

@@ -12,9 +12,10 @@
 //
 // What bounds it: many rows, the matrix cores beside the vector unit (128 elements a row: 512 operations of the one for each exponential,
 // sum and rounding of the other), and the power they draw.  8 x 32 heads x 4096 x 128 bf16, causal: 1180 us, 930 TFLOP/s (a product of
-// 8192^3: 1155 to 1394); with a position bias, far tiles left out, 887; 8 heads of 8 x 512 rows at the end of 8192 keys 500 us, 1070 TFLOP/s; 256
-// elements 760, 64 elements 760, fp32 59 (its own products' rate).  Counters: no bank conflicts in LDS, matrix cores busy 40 % of the cycles at 2.0
-// GHz; inputs of zeros run 10 % faster.  Few rows: the chain of a walk, 8 us for 1000 keys, and the join; 16 x 2048 x 128 40 us.
+// 8192^3: 1155 to 1394); with a position bias, far tiles left out, 887; 8 heads of 8 x 512 rows at the end of 8192 keys 511 us, 1045 TFLOP/s; 256
+// elements 760 (one wave a SIMD: a third of its cycles wait for data or a barrier), 64 elements 765 (the vector unit is busy two thirds of the
+// cycles, the matrix cores one), fp32 79 (a product of 8192^3: 154).  Counters: no bank conflicts in LDS; 128 elements: matrix cores and vector unit
+// each busy 45 % of the cycles; inputs of zeros run 18 % faster, which is power.  Few rows: the chain of a walk, 8 us for 1000 keys, and the join; 16 x 2048 x 128 40 us.
 //
 // Steps of 8 x 32 x 4096 x 128: tiles by way of registers, which spilled, 3133 us; infinities and NaNs of edge tiles taken out in LDS instead
 // of beside every product 1328; direct loads to LDS 1245; keys a step ahead of the values 1190.  Tried, no gain: tiles of 32 keys (3 to 5 % more),
